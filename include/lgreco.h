@@ -18,6 +18,9 @@
  *   lgreco_compress  apply the chosen per-layer setting, produce the payload and update
  *                    the error-feedback buffer (what the paper's communication engine does
  *                    with the mapping, section "Implementation")
+ *   lgreco_optim_*   what follows the exchange on every worker: squared norms of the layers'
+ *                    gradients, clipping, and the AdamW step over all layers, with moments in
+ *                    fp32 or in 8 bits
  *
  * Three compression families (section "Experimental Validation"): bucketed quantization
  * with b bits per value, layer-wise Top-K with density d, PowerSGD-style low rank with rank r.
@@ -382,6 +385,111 @@ int64_t lgreco_late_handovers(const lgreco_handle_t* h);
  * had to be resolved by Algorithm 1's tie-breaks, -G sequentially after that resolution gave up.
  * Diagnostics only. */
 int lgreco_last_solve_groups(const lgreco_handle_t* h);
+
+/* ------------------------------------------------------------------ the optimizer step
+ * AdamW with decoupled weight decay over all layers of a table in one pass, behind
+ * lgreco_decompress.  A plan holds what such calls need of the layer table; it is independent of the
+ * compression's handle, whose table may list other layers of the same buffers (tensors that
+ * travel uncompressed still have to be stepped).
+ *
+ * A plan never changes after its creation, and its calls read nothing from the host after they
+ * return, allocate nothing, wait for nothing and read no other host memory than their arguments:
+ * all outputs are complete in stream order, and every call may be captured into a HIP graph.  A
+ * replay repeats the call with the host arguments it was captured with (the settings) on the
+ * buffers it was captured with; the step count and the learning rate's factor are read from the
+ * device.  Calls on one plan share its scratch: they, and replays of graphs that hold them, must not
+ * overlap in time.  A plan is used with the device current that was current at its creation (another
+ * one: LGRECO_EINVAL), and destroyed when none of its calls or graphs is in use any more.
+ *
+ * The buffers d_grads, d_params, d_m, d_v and d_copy have the layout of the table: layer l is
+ * the elements [offset, offset + numel) of each.  They must not overlap.  Elements outside the
+ * layers are neither read nor written.  A buffer starts at a multiple of its element's size. */
+typedef struct lgreco_optim lgreco_optim_t;
+
+#define LGRECO_F32  0
+#define LGRECO_BF16 1
+#define LGRECO_F16  2
+
+#define LGRECO_OPTIM_BLOCK 128   /* elements that share the exponents of 8-bit moments */
+
+typedef struct {
+    double   lr;            /* >= 0 */
+    double   beta1, beta2;  /* in [0, 1) */
+    double   eps;           /* positive, also as fp32 */
+    double   weight_decay;  /* >= 0 */
+    double   grad_scale;    /* every gradient is multiplied by it first: 1 / workers behind a sum of their
+                             * gradients, 1 / loss scale; > 0 */
+    double   max_norm;      /* > 0: gradients are clipped to this global norm (after grad_scale); 0: not */
+    uint64_t seed;          /* of the stochastic rounding */
+    int32_t  stochastic;    /* 8-bit moments: 0 round to nearest, ties to even codes; 1 stochastically */
+    int32_t  reserved;      /* must be 0 */
+} lgreco_adamw_t;
+
+/* Creates a plan for these layers on the current device (48 bytes for every 1024 elements of device memory,
+ * or less).
+ *   lr_scale     host [L] factors of lr per layer, or NULL (= 1): finite, >= 0
+ *   decay_scale  host [L] factors of weight_decay per layer, or NULL (= 1): finite, >= 0 */
+int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int32_t L, const float* lr_scale,
+                        const float* decay_scale);
+int lgreco_optim_destroy(lgreco_optim_t* o);
+
+/* Blocks of the plan's layers: sum over layers of ceil(numel / LGRECO_OPTIM_BLOCK); -1 for NULL. */
+int64_t lgreco_optim_blocks(const lgreco_optim_t* o);
+
+/* Squared norms of the gradients as they are (before any grad_scale).
+ *   grad_type  LGRECO_F32 or LGRECO_BF16
+ *   d_sumsq    device out [L + 1], fp64: [l] sum of the squares of layer l, [L] sum over all layers.  Summed in
+ *              fp64 in an order that only depends on the table: two calls give the same bits.  A NaN or an
+ *              infinity among the gradients makes the layer's sum and the last one NaN or infinite. */
+int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type, double* d_sumsq, void* stream);
+
+/* One step.  With t = *d_step + 1, c = grad_scale * min(1, max_norm / (grad_scale * sqrt(S) + 1e-6)), S = d_sumsq[L]
+ * (c = grad_scale without clipping), lr_l = lr * *d_lr * lr_scale[l] and wd_l = weight_decay * decay_scale[l]:
+ *   g = c * grad;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + (1 - beta2) g^2
+ *   p' = p - lr_l wd_l p - lr_l / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+ * in fp32, the factors that are the same for all elements in fp64.
+ *   grad_type  LGRECO_F32 or LGRECO_BF16
+ *   d_params   fp32, in/out;   d_m, d_v  fp32 moments, in/out (zero before the first step)
+ *   d_copy     out: p' rounded to nearest even in copy_type (LGRECO_BF16 or LGRECO_F16; fp16: beyond
+ *              65504 infinite), or NULL
+ *   d_sumsq    the array lgreco_optim_norms filled (or the same summed over shards), or NULL.  When S is
+ *              NaN or infinite, the step is left out: no buffer and no step count changes.
+ *              Required with max_norm > 0.
+ *   d_lr       fp32 on the device, multiplies lr (a schedule that replays follow), or NULL (= 1)
+ *   d_step     int64 on the device: steps taken so far, in/out */
+int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
+                       float* d_params, float* d_m, float* d_v, void* d_copy, int32_t copy_type,
+                       const double* d_sumsq, const float* d_lr, int64_t* d_step, void* stream);
+
+/* The same step with moments in 8 bits, 2 bytes an element instead of 8.  A block of 128 consecutive
+ * elements, counted from its layer's start (the last one of a layer may be shorter), shares two exponents.
+ *   d_m      uint8: sign (bit 7) and magnitude of m;   d_v  uint8: v; both laid out as the gradients are
+ *   d_exps   uint8 [2 x blocks]: exponents of m and of v of every block, the layers' blocks one after another
+ * All of them zero before the first step.  The value of a code c with exponent x is the fp32 number with the bits
+ * (c & 127) << 19 times 2^(x - 7) for m, with its sign, and the one with the bits c << 19 times 2^(x - 15) for v: four
+ * bits of mantissa behind the leading one, over 7 and 15 octaves, and evenly spaced codes below those.  x is
+ * the biased fp32 exponent of the block's largest magnitude, one more where its mantissa exceeds 31/16, so that no
+ * code saturates.  A v that is not zero never becomes the code 0 (whose element would be stepped as if its
+ * gradient had been 0 forever).  The parameters are updated from m' and v' before they are rounded.
+ * Rounding to nearest keeps a v whose relative change in a step is below 1/32, in the uppermost octaves, where it was: with
+ * beta2 = 0.999 it hardly ever falls.  Stochastic rounding is free of that: up with the probability that keeps the
+ * expectation, from word (i mod 4) of Philox4x32-10 keyed by seed at the counter (i / 4, t, l, 1) (t modulo 2^32, its upper
+ * half added to the 1), i the element's index within layer l; m takes the lower 16 bits, v the upper ones.
+ * NaN or infinite gradients, where d_sumsq is not there to leave the step out, give undefined moments in their blocks (never a fault). */
+int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
+                             float* d_params, uint8_t* d_m, uint8_t* d_v, uint8_t* d_exps, void* d_copy,
+                             int32_t copy_type, const double* d_sumsq, const float* d_lr, int64_t* d_step,
+                             void* stream);
+
+/* The values of 8-bit moments, for inspection or a change to fp32 moments.
+ *   type            LGRECO_F32, or LGRECO_BF16 (exact too, but for magnitudes below 2^-126)
+ *   d_m_out, d_v_out  out, in that type, laid out as the gradients are; elements outside the layers are
+ *                   not written */
+int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_v, const uint8_t* d_exps,
+                        void* d_m_out, void* d_v_out, int32_t type, void* stream);
+
+/* Text of the last HIP error seen by this plan ("" if none). */
+const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o);
 
 const char* lgreco_strerror(int status);
 /* Text of the last HIP error seen by this handle ("" if none). */

@@ -17,13 +17,17 @@ LIB_PATH = os.path.join(_HERE, "liblgreco.so")
 
 OK, EINVAL, ENOSPACE, EINFEASIBLE, EHIP, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 QUANT, TOPK, LOWRANK = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
+OPTIM_BLOCK = 128
 CALL_PROFILE, CALL_SOLVE, CALL_COMPRESS, CALL_RECEIVE = 0, 1, 2, 3
 
 EXPORTS = ("lgreco_create", "lgreco_destroy", "lgreco_sizes", "lgreco_profile", "lgreco_profile_solve", "lgreco_profile_solve_compress",
            "lgreco_candidate_range", "lgreco_emax",
            "lgreco_solve", "lgreco_solve_static", "lgreco_solve_weighted", "lgreco_payload_layout", "lgreco_compress", "lgreco_decompress", "lgreco_accumulate", "lgreco_set_timing", "lgreco_set_timing_stride",
            "lgreco_get_timing", "lgreco_get_timing_of", "lgreco_get_timing_totals", "lgreco_strerror", "lgreco_last_hip_error", "lgreco_last_solve_groups",
-           "lgreco_set_ef_zero_on_entry", "lgreco_late_handovers")
+           "lgreco_set_ef_zero_on_entry", "lgreco_late_handovers",
+           "lgreco_optim_create", "lgreco_optim_destroy", "lgreco_optim_blocks", "lgreco_optim_norms", "lgreco_optim_adamw",
+           "lgreco_optim_adamw_coded", "lgreco_optim_decode", "lgreco_optim_last_hip_error")
 
 
 class Layer(C.Structure):
@@ -39,6 +43,12 @@ class Config(C.Structure):
                 ("power_iters", C.c_int32), ("r_max", C.c_int32), ("reuse_thresholds", C.c_int32),
                 ("dp_groups", C.c_int32), ("strict_budget", C.c_int32),
                 ("keep_ef_on_failure", C.c_int32)]
+
+
+class AdamW(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("max_norm", C.c_double),
+                ("seed", C.c_uint64), ("stochastic", C.c_int32), ("reserved", C.c_int32)]
 
 
 class LgrecoError(RuntimeError):
@@ -93,6 +103,16 @@ def lib() -> C.CDLL:
         l.lgreco_late_handovers.restype = C.c_int64
         l.lgreco_last_hip_error.argtypes = [vp]
         l.lgreco_last_hip_error.restype = C.c_char_p
+        l.lgreco_optim_create.argtypes = [C.POINTER(vp), vp, i32, vp, vp]
+        l.lgreco_optim_destroy.argtypes = [vp]
+        l.lgreco_optim_blocks.argtypes = [vp]
+        l.lgreco_optim_blocks.restype = C.c_int64
+        l.lgreco_optim_norms.argtypes = [vp, vp, i32, vp, vp]
+        l.lgreco_optim_adamw.argtypes = [vp, C.POINTER(AdamW), vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        l.lgreco_optim_adamw_coded.argtypes = [vp, C.POINTER(AdamW), vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        l.lgreco_optim_decode.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp]
+        l.lgreco_optim_last_hip_error.argtypes = [vp]
+        l.lgreco_optim_last_hip_error.restype = C.c_char_p
         for name in EXPORTS:
             if getattr(l, name).restype is C.c_int:
                 pass
@@ -360,3 +380,98 @@ class Handle:
         if n < 0:
             self._check(n)
         return [(names[i].decode(), float(ms[i]), int(cnt[i])) for i in range(min(n, cap))]
+
+
+def adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+          grad_scale: float = 1.0, max_norm: float = 0.0, stochastic: bool = False, seed: int = 0) -> AdamW:
+    """Settings of a step (lgreco_adamw_t)."""
+    return AdamW(lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm, seed & (2 ** 64 - 1), int(bool(stochastic)), 0)
+
+
+class Optim:
+    """lgreco_optim_t with the entry points as methods: the optimizer step over the layers of one table.  Tensors have
+    the table's layout (flat, contiguous, on the plan's device, at least `extent` elements)."""
+
+    def __init__(self, layers, lr_scale: Optional[Sequence[float]] = None, decay_scale: Optional[Sequence[float]] = None):
+        import torch
+        self._o = C.c_void_p()
+        scales = []
+        for a in (lr_scale, decay_scale):
+            a = None if a is None else np.ascontiguousarray(a, np.float32)
+            if a is not None and a.shape != (len(layers),):
+                raise ValueError("one factor per layer")
+            scales.append(a)
+        self.device = torch.cuda.current_device()
+        st = lib().lgreco_optim_create(C.byref(self._o), C.addressof(layers), len(layers),
+                                       *(None if a is None else _np(a) for a in scales))
+        if st != OK:
+            raise LgrecoError(st, strerror(st))
+        self.L = len(layers)
+        self.extent = max(a.offset + a.numel for a in layers)
+        self.blocks = int(lib().lgreco_optim_blocks(self._o))
+        self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        self._f32, self._f64, self._u8, self._i64 = torch.float32, torch.float64, torch.uint8, torch.int64
+
+    def close(self):
+        if self._o:
+            lib().lgreco_optim_destroy(self._o)
+            self._o = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int):
+        if st != OK:
+            text = strerror(st)
+            if st == EHIP:
+                text += " (" + lib().lgreco_optim_last_hip_error(self._o).decode() + ")"
+            raise LgrecoError(st, text)
+
+    def _ptr(self, t, dtype, numel: int) -> Optional[int]:
+        """Device address of a tensor that has to be of this type (None: one of the floating types a call takes) and size."""
+        if t is None:
+            return None
+        if not t.is_cuda or not t.is_contiguous() or t.get_device() != self.device:
+            raise ValueError("expected a contiguous tensor on the plan's device")
+        if (t.dtype is not dtype) if dtype is not None else (t.dtype not in self._types):
+            raise ValueError("unexpected tensor type %s" % t.dtype)
+        if t.numel() < numel:
+            raise ValueError("the tensor has %d elements, the layers reach to %d" % (t.numel(), numel))
+        return t.data_ptr()
+
+    def norms(self, d_grads, d_sumsq, stream=None):
+        """d_sumsq (fp64, layers + 1): squared norm of every layer's gradient, then of all together."""
+        self._check(lib().lgreco_optim_norms(self._o, self._ptr(d_grads, None, self.extent), self._types[d_grads.dtype],
+                                             self._ptr(d_sumsq, self._f64, self.L + 1), _stream(stream)))
+
+    def adamw(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_step, d_copy=None, d_sumsq=None, d_lr=None, stream=None):
+        """One step with fp32 moments; gradients fp32 or bf16, d_copy (bf16 or fp16) receives the parameters too."""
+        n = self.extent
+        self._check(lib().lgreco_optim_adamw(
+            self._o, C.byref(settings), self._ptr(d_grads, None, n), self._types[d_grads.dtype], self._ptr(d_params, self._f32, n),
+            self._ptr(d_m, self._f32, n), self._ptr(d_v, self._f32, n), self._ptr(d_copy, None, n),
+            0 if d_copy is None else self._types[d_copy.dtype], self._ptr(d_sumsq, self._f64, self.L + 1),
+            self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1), _stream(stream)))
+
+    def adamw_coded(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_exps, d_step, d_copy=None, d_sumsq=None, d_lr=None,
+                    stream=None):
+        """One step with moments in 8 bits: d_m, d_v uint8 codes, d_exps uint8 (2 * blocks) exponents."""
+        n = self.extent
+        self._check(lib().lgreco_optim_adamw_coded(
+            self._o, C.byref(settings), self._ptr(d_grads, None, n), self._types[d_grads.dtype], self._ptr(d_params, self._f32, n),
+            self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
+            self._ptr(d_copy, None, n), 0 if d_copy is None else self._types[d_copy.dtype],
+            self._ptr(d_sumsq, self._f64, self.L + 1), self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1),
+            _stream(stream)))
+
+    def decode(self, d_m, d_v, d_exps, d_m_out, d_v_out, stream=None):
+        """Values of 8-bit moments, both outputs fp32 or both bf16."""
+        n = self.extent
+        if d_m_out.dtype is not d_v_out.dtype:
+            raise ValueError("outputs of one type")
+        self._check(lib().lgreco_optim_decode(
+            self._o, self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
+            self._ptr(d_m_out, None, n), self._ptr(d_v_out, None, n), self._types[d_m_out.dtype], _stream(stream)))

@@ -234,23 +234,6 @@ int check_cand(const lgreco_cand_t& c, const lgreco_layer_t* layer, int r_max) {
     }
 }
 
-int check_layers(const lgreco_layer_t* layers, int32_t L) {
-    if (!layers || L <= 0) return LGRECO_EINVAL;
-    std::vector<std::pair<int64_t, int64_t>> r;
-    r.reserve(L);
-    for (int l = 0; l < L; ++l) {
-        const lgreco_layer_t& a = layers[l];
-        if (a.offset < 0 || a.numel <= 0 || a.numel >= ((int64_t)1 << 31)) return LGRECO_EINVAL;
-        if (a.rows < 0 || a.cols < 0) return LGRECO_EINVAL;
-        if (a.rows > 0 && (int64_t)a.rows * a.cols != a.numel) return LGRECO_EINVAL;
-        r.emplace_back(a.offset, a.offset + a.numel);
-    }
-    std::sort(r.begin(), r.end());
-    for (int l = 1; l < L; ++l)
-        if (r[l].first < r[l - 1].second) return LGRECO_EINVAL;
-    return LGRECO_OK;
-}
-
 bool some_topk(const lgreco_cand_t* cands, int32_t P) {
     return std::any_of(cands, cands + P, [](const lgreco_cand_t& c) { return c.family == LGRECO_TOPK; });
 }
@@ -467,6 +450,23 @@ void record_dp_sub(lgreco_handle* h) {
 }
 
 }  // namespace
+
+int lgreco::check_layers(const lgreco_layer_t* layers, int32_t L) {
+    if (!layers || L <= 0) return LGRECO_EINVAL;
+    std::vector<std::pair<int64_t, int64_t>> r;
+    r.reserve(L);
+    for (int l = 0; l < L; ++l) {
+        const lgreco_layer_t& a = layers[l];
+        if (a.offset < 0 || a.numel <= 0 || a.numel >= ((int64_t)1 << 31)) return LGRECO_EINVAL;
+        if (a.rows < 0 || a.cols < 0) return LGRECO_EINVAL;
+        if (a.rows > 0 && (int64_t)a.rows * a.cols != a.numel) return LGRECO_EINVAL;
+        r.emplace_back(a.offset, a.offset + a.numel);
+    }
+    std::sort(r.begin(), r.end());
+    for (int l = 1; l < L; ++l)
+        if (r[l].first < r[l - 1].second) return LGRECO_EINVAL;
+    return LGRECO_OK;
+}
 
 extern "C" {
 

@@ -11,6 +11,9 @@
 
 namespace lgreco {
 
+// LGRECO_OK when a layer table is what the entry points take: sizes in range, no two layers overlap.
+int check_layers(const lgreco_layer_t* layers, int32_t L);
+
 // Optional per-kernel timing.  A Section covers the work enqueued during its lifetime with two HIP
 // events of the call's stream.  A main-kernel section (the level-1 sections a benchmark keeps on
 // inside its timed region) puts its events on the kernels themselves: launch_timed below hands

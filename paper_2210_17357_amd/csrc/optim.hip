@@ -1,0 +1,608 @@
+// The optimizer step behind the exchange of gradients: squared norms of the layers' gradients, and AdamW over
+// all layers with moments in fp32 or in 8 bits.  gfx950 / wave64.
+//
+// AdamW (Loshchilov, Hutter: decoupled weight decay), element by element, c the gradients' common factor:
+//   g = c * grad;  m' = b1 m + (1 - b1) g;  v' = b2 v + (1 - b2) g^2
+//   p' = p - lr wd p - (lr / (1 - b1^t)) m' / (sqrt(v') / sqrt(1 - b2^t) + eps)
+// Everything here streams: nothing is read twice, all kernels are bound by HBM on large tables and by launches on small ones.
+#include <cfloat>
+#include <cmath>
+#include <cstdio>
+#include <limits>
+#include <new>
+#include <vector>
+
+#include "internal.h"
+
+namespace lgreco {
+namespace {
+
+constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
+constexpr int kNormPart = 16384;     // elements of a workgroup of the norms
+constexpr int kStepPart = 2048;      // elements of a workgroup of the step
+constexpr int kLine = 32;            // elements of a 128-byte line of fp32
+
+// What one workgroup works on: consecutive elements of one layer.
+struct Part {
+    int64_t start;       // first element, into the flat buffers
+    int64_t block;       // 8-bit moments: its first block
+    int32_t count;       // elements
+    int32_t pos;         // first element, relative to the layer start
+    int32_t layer;
+    float lr_scale, decay_scale;
+    int32_t pad;
+};
+
+// The step's factors that are the same for all elements, worked out on the device (the step count, the norm and the
+// learning rate's factor lie there).
+struct StepFactors {
+    double lr;           // lr * *d_lr
+    double lr_m;         // the same over 1 - b1^t
+    float grad;          // factor of the gradients
+    float root_v;        // 1 / sqrt(1 - b2^t)
+    uint32_t t_lo, t_hi; // t
+    int32_t go;          // 0: the step is left out
+    int32_t pad[3];
+};
+
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+struct BF16 { uint16_t bits; };
+struct F16 { uint16_t bits; };
+struct NoCopy { };
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(BF16 x) { return __builtin_bit_cast(float, (uint32_t)x.bits << 16); }
+__device__ __forceinline__ uint16_t narrow_bits(float x, BF16) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint16_t narrow_bits(float x, F16) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+
+__device__ __forceinline__ float4 load4(const float* p) { return load_stream(p); }
+__device__ __forceinline__ float4 load4(const BF16* p) {
+    const u16x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
+    return make_float4(widen(BF16{v.x}), widen(BF16{v.y}), widen(BF16{v.z}), widen(BF16{v.w}));
+}
+template <typename C>
+__device__ __forceinline__ void store4(C* p, const float4 v) {
+    u16x4_any n;
+    n.x = narrow_bits(v.x, C{}); n.y = narrow_bits(v.y, C{}); n.z = narrow_bits(v.z, C{}); n.w = narrow_bits(v.w, C{});
+    __builtin_nontemporal_store(n, reinterpret_cast<u16x4_any*>(p));
+}
+__device__ __forceinline__ void store4(float* p, const float4 v) { store_stream(p, v); }
+__device__ __forceinline__ void store4(NoCopy*, const float4) {}
+template <typename C>
+__device__ __forceinline__ void store1(C* p, float v) { p->bits = narrow_bits(v, C{}); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(NoCopy*, float) {}
+template <typename C>
+__device__ __forceinline__ C* shifted(C* p, int64_t n) { return p + n; }
+__device__ __forceinline__ NoCopy* shifted(NoCopy* p, int64_t) { return p; }
+
+// ------------------------------------------------------------------ norms
+template <typename G>
+__global__ __launch_bounds__(kThreads) void norm_part_kernel(const Part* __restrict__ parts, const G* __restrict__ grads,
+                                                             double* __restrict__ partials) {
+    __shared__ double s_sum[kThreads / 64];
+    const Part t = parts[blockIdx.x];
+    const G* const g = grads + t.start;
+    const int tid = threadIdx.x;
+    double a0 = 0.0, a1 = 0.0, a2 = 0.0, a3 = 0.0;
+#pragma unroll 4
+    for (int i = 4 * tid; i + 4 <= t.count; i += 4 * kThreads) {
+        const float4 x = load4(g + i);
+        a0 = __builtin_fma((double)x.x, (double)x.x, a0);
+        a1 = __builtin_fma((double)x.y, (double)x.y, a1);
+        a2 = __builtin_fma((double)x.z, (double)x.z, a2);
+        a3 = __builtin_fma((double)x.w, (double)x.w, a3);
+    }
+    if (tid < (t.count & 3)) {
+        const double x = (double)widen(g[(t.count & ~3) + tid]);
+        a0 = __builtin_fma(x, x, a0);
+    }
+    const double w = wave_sum((a0 + a1) + (a2 + a3));
+    if ((tid & 63) == 0) s_sum[tid >> 6] = w;
+    __syncthreads();
+    if (tid == 0) partials[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+
+// Sum of n doubles in an order that depends on n alone, one workgroup.
+__device__ __forceinline__ void sum_block(const double* __restrict__ x, int n, double* out) {
+    __shared__ double s_sum[kThreads / 64];
+    const int tid = threadIdx.x;
+    double a = 0.0;
+    for (int i = tid; i < n; i += kThreads) a += x[i];
+    const double w = wave_sum(a);
+    if ((tid & 63) == 0) s_sum[tid >> 6] = w;
+    __syncthreads();
+    if (tid == 0) *out = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+
+__global__ __launch_bounds__(kThreads) void norm_layer_kernel(const double* __restrict__ partials, const int32_t* __restrict__ begin,
+                                                              double* __restrict__ sumsq) {
+    const int b = begin[blockIdx.x];
+    sum_block(partials + b, begin[blockIdx.x + 1] - b, sumsq + blockIdx.x);
+}
+__global__ __launch_bounds__(kThreads) void norm_total_kernel(double* __restrict__ sumsq, int n) { sum_block(sumsq, n, sumsq + n); }
+
+// ------------------------------------------------------------------ the step's factors
+struct FactorParams {
+    double lr, beta1, beta2, grad_scale, max_norm;
+    const double* total;     // sum of the squared gradients, or null
+    const float* lr_factor;  // or null
+    int64_t* step;
+    StepFactors* out;
+};
+
+__global__ __launch_bounds__(64) void factors_kernel(FactorParams p) {
+    if (threadIdx.x != 0) return;
+    StepFactors f{};
+    double c = p.grad_scale;
+    f.go = 1;
+    if (p.total) {
+        const double s = *p.total;
+        if (!(s <= DBL_MAX)) f.go = 0;                           // NaN or infinite
+        if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * sqrt(s) + 1e-6));
+    }
+    const int64_t t = *p.step + 1;
+    f.lr = p.lr_factor ? p.lr * (double)*p.lr_factor : p.lr;
+    f.lr_m = f.lr / (1.0 - pow(p.beta1, (double)t));
+    f.root_v = (float)(1.0 / sqrt(1.0 - pow(p.beta2, (double)t)));
+    f.grad = (float)c;
+    f.t_lo = (uint32_t)t;
+    f.t_hi = (uint32_t)((uint64_t)t >> 32);
+    *p.out = f;
+    if (f.go) *p.step = t;
+}
+
+// ------------------------------------------------------------------ AdamW
+struct StepParams {
+    const Part* parts;
+    const StepFactors* factors;
+    const void* grads;
+    float* p;
+    void* m;
+    void* v;
+    uint8_t* exps;
+    void* copy;
+    double weight_decay;
+    float beta1, rest1, beta2, rest2, eps;     // rest = 1 - beta
+    int32_t stochastic;
+    uint32_t seed_lo, seed_hi;
+};
+
+// The factors of one layer's elements.
+struct Rates {
+    float shrink;        // lr wd
+    float rate;          // lr / (1 - b1^t)
+    float grad, root_v;
+};
+__device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams& p, const Part& t) {
+    const double s = (double)t.lr_scale;
+    return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v};
+}
+
+__device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, float grad, float& p, float& m, float& v) {
+    const float g = r.grad * grad;
+    m = __builtin_fmaf(k.beta1, m, k.rest1 * g);
+    v = __builtin_fmaf(k.beta2, v, k.rest2 * (g * g));
+    const float u = m / __builtin_fmaf(sqrtf(v), r.root_v, k.eps);
+    p -= __builtin_fmaf(r.shrink, p, r.rate * u);
+}
+
+template <typename G, typename C>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
+    const StepFactors f = *k.factors;
+    if (!f.go) return;
+    const Part t = k.parts[blockIdx.x];
+    const Rates r = rates_of(f, k, t);
+    const G* const g = static_cast<const G*>(k.grads) + t.start;
+    float* const p = k.p + t.start;
+    float* const m = static_cast<float*>(k.m) + t.start;
+    float* const v = static_cast<float*>(k.v) + t.start;
+    C* const copy = shifted(static_cast<C*>(k.copy), t.start);
+    const int tid = threadIdx.x;
+    for (int i = 4 * tid; i + 4 <= t.count; i += 4 * kThreads) {
+        const float4 gi = load4(g + i);
+        float4 pi = load4(p + i), mi = load4(m + i), vi = load4(v + i);
+        step_one(k, r, gi.x, pi.x, mi.x, vi.x);
+        step_one(k, r, gi.y, pi.y, mi.y, vi.y);
+        step_one(k, r, gi.z, pi.z, mi.z, vi.z);
+        step_one(k, r, gi.w, pi.w, mi.w, vi.w);
+        store4(p + i, pi);
+        store4(m + i, mi);
+        store4(v + i, vi);
+        store4(copy + (__is_same(C, NoCopy) ? 0 : i), pi);
+    }
+    if (tid < (t.count & 3)) {
+        const int i = (t.count & ~3) + tid;
+        float pi = p[i], mi = m[i], vi = v[i];
+        step_one(k, r, widen(g[i]), pi, mi, vi);
+        p[i] = pi;
+        m[i] = mi;
+        v[i] = vi;
+        store1(copy + (__is_same(C, NoCopy) ? 0 : i), pi);
+    }
+}
+
+// ------------------------------------------------------------------ 8-bit moments
+// A magnitude a of a block whose exponent byte is x is held as the bits 19.. of the fp32 number a 2^(top - x), top = 7 for m and
+// 15 for v: exponent field and 4 bits of mantissa in one small whole number, denormal numbers as the evenly spaced
+// codes below the lowest octave.
+constexpr int kTopM = 7, kTopV = 15, kCodeShift = 19;
+
+__device__ __forceinline__ float decoded_m(uint32_t code, int x) {
+    return __builtin_ldexpf(__builtin_bit_cast(float, (code & 127u) << kCodeShift | (code & 128u) << 24), x - kTopM);
+}
+__device__ __forceinline__ float decoded_v(uint32_t code, int x) {
+    return __builtin_ldexpf(__builtin_bit_cast(float, code << kCodeShift), x - kTopV);
+}
+
+// The exponent byte of a block whose largest magnitude has these bits: its exponent, one more where rounding to 4 bits of
+// mantissa could carry into the next octave.
+__device__ __forceinline__ int block_exponent(uint32_t bits) { return (int)((bits + ((1u << kCodeShift) - 1)) >> 23); }
+
+// r: 16 random bits.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t encoded(float a, int shift, uint32_t r) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_ldexpf(a, shift));
+    const uint32_t add = STOCHASTIC ? (r << 3 | 4u) : ((1u << (kCodeShift - 1)) - 1) + (b >> kCodeShift & 1u);
+    return (b + add) >> kCodeShift;
+}
+
+__device__ __forceinline__ uint32_t row16_umax(uint32_t v) {
+    v = max(v, dpp_u32<kDppQuadXor1>(v));
+    v = max(v, dpp_u32<kDppQuadXor2>(v));
+    v = max(v, dpp_u32<kDppRowHalfMirror>(v));
+    v = max(v, dpp_u32<kDppRowMirror>(v));
+    return v;
+}
+
+// A thread takes 8 consecutive elements and a row of 16 lanes a block, so that the block's maxima take four vector
+// instructions each and no LDS.
+template <typename G, typename C, bool STOCHASTIC>
+__global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
+    const StepFactors f = *k.factors;
+    if (!f.go) return;
+    const Part t = k.parts[blockIdx.x];
+    const Rates r = rates_of(f, k, t);
+    const int i = 8 * threadIdx.x, left = t.count - i;
+    const G* const g = static_cast<const G*>(k.grads) + t.start + i;
+    float* const p = k.p + t.start + i;
+    uint8_t* const m = static_cast<uint8_t*>(k.m) + t.start + i;
+    uint8_t* const v = static_cast<uint8_t*>(k.v) + t.start + i;
+    C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
+    uint8_t* const exps = k.exps + 2 * (t.block + i / kOptimBlock);
+
+    float gi[8], pi[8], mi[8], vi[8];
+    uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
+    int xm = 0, xv = 0;
+    if (left > 0) {
+        xm = exps[0];
+        xv = exps[1];
+    }
+    if (left >= 8) {
+        const float4 ga = load4(g), gb = load4(g + 4), pa = load4(p), pb = load4(p + 4);
+        const u32x2_any a = *reinterpret_cast<const u32x2_any*>(m), b = *reinterpret_cast<const u32x2_any*>(v);
+        cm[0] = a.x; cm[1] = a.y; cv[0] = b.x; cv[1] = b.y;
+        gi[0] = ga.x; gi[1] = ga.y; gi[2] = ga.z; gi[3] = ga.w; gi[4] = gb.x; gi[5] = gb.y; gi[6] = gb.z; gi[7] = gb.w;
+        pi[0] = pa.x; pi[1] = pa.y; pi[2] = pa.z; pi[3] = pa.w; pi[4] = pb.x; pi[5] = pb.y; pi[6] = pb.z; pi[7] = pb.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = j < left;
+            gi[j] = in ? widen(g[j]) : 0.0f;
+            pi[j] = in ? p[j] : 0.0f;
+            cm[j >> 2] |= in ? (uint32_t)m[j] << 8 * (j & 3) : 0u;
+            cv[j >> 2] |= in ? (uint32_t)v[j] << 8 * (j & 3) : 0u;
+        }
+    }
+    // (elements past the layer's end: gradient 0 and codes 0, so their moments are 0)
+    uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        mi[j] = decoded_m(cm[j >> 2] >> 8 * (j & 3) & 255u, xm);
+        vi[j] = decoded_v(cv[j >> 2] >> 8 * (j & 3) & 255u, xv);
+        step_one(k, r, gi[j], pi[j], mi[j], vi[j]);
+        top_m = max(top_m, __builtin_bit_cast(uint32_t, mi[j]) & 0x7FFFFFFFu);
+        top_v = max(top_v, __builtin_bit_cast(uint32_t, vi[j]));
+    }
+    xm = min(block_exponent(row16_umax(top_m)), 255);
+    xv = min(block_exponent(row16_umax(top_v)), 255);
+    Philox4 words[2] = {};
+    if (STOCHASTIC) {
+        const uint32_t quad = (uint32_t)(t.pos + i) / 4;
+        words[0] = philox4x32_10(quad, f.t_lo, (uint32_t)t.layer, 1u + f.t_hi, k.seed_lo, k.seed_hi);
+        words[1] = philox4x32_10(quad + 1, f.t_lo, (uint32_t)t.layer, 1u + f.t_hi, k.seed_lo, k.seed_hi);
+    }
+    cm[0] = cm[1] = cv[0] = cv[1] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t w = words[j >> 2].w[j & 3];
+        const uint32_t sign = __builtin_bit_cast(uint32_t, mi[j]) >> 31 << 7;
+        const uint32_t a = min(encoded<STOCHASTIC>(__builtin_fabsf(mi[j]), kTopM - xm, w & 0xFFFFu), 127u) | sign;
+        const uint32_t b = max(min(encoded<STOCHASTIC>(vi[j], kTopV - xv, w >> 16), 255u), vi[j] > 0.0f ? 1u : 0u);
+        cm[j >> 2] |= a << 8 * (j & 3);
+        cv[j >> 2] |= b << 8 * (j & 3);
+    }
+    if (left <= 0) return;
+    if ((threadIdx.x & 15) == 0) {
+        exps[0] = (uint8_t)xm;
+        exps[1] = (uint8_t)xv;
+    }
+    if (left >= 8) {
+        u32x2_any a, b;
+        a.x = cm[0]; a.y = cm[1]; b.x = cv[0]; b.y = cv[1];
+        *reinterpret_cast<u32x2_any*>(m) = a;
+        *reinterpret_cast<u32x2_any*>(v) = b;
+        const float4 pa = make_float4(pi[0], pi[1], pi[2], pi[3]), pb = make_float4(pi[4], pi[5], pi[6], pi[7]);
+        store4(p, pa);
+        store4(p + 4, pb);
+        store4(copy, pa);
+        store4(shifted(copy, 4), pb);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j < left) {
+                p[j] = pi[j];
+                m[j] = (uint8_t)(cm[j >> 2] >> 8 * (j & 3));
+                v[j] = (uint8_t)(cv[j >> 2] >> 8 * (j & 3));
+                store1(shifted(copy, j), pi[j]);
+            }
+        }
+    }
+}
+
+template <typename O>
+__global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restrict__ parts, const uint8_t* __restrict__ codes_m,
+                                                           const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
+                                                           O* __restrict__ m_out, O* __restrict__ v_out) {
+    const Part t = parts[blockIdx.x];
+    const uint8_t* const m = codes_m + t.start;
+    const uint8_t* const v = codes_v + t.start;
+    const uint8_t* const x = exps + 2 * t.block;
+    for (int i = threadIdx.x; i < t.count; i += kThreads) {
+        store1(m_out + t.start + i, decoded_m(m[i], x[2 * (i / kOptimBlock)]));
+        store1(v_out + t.start + i, decoded_v(v[i], x[2 * (i / kOptimBlock) + 1]));
+    }
+}
+
+// A launch's own error, whatever another call on this thread left behind.
+template <typename... A>
+hipError_t launch(void (*kernel)(A...), int64_t grid, int threads, hipStream_t s, A... args) {
+    void* list[] = {&args...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), list, 0, s);
+}
+
+size_t element_size(int32_t type) { return type == LGRECO_F32 ? 4 : 2; }
+bool misaligned(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
+
+}  // namespace
+}  // namespace lgreco
+
+using namespace lgreco;
+
+struct lgreco_optim {
+    int device = 0;
+    int32_t L = 0;
+    int64_t blocks = 0;
+    int64_t n_norm = 0, n_step = 0, n_coded = 0;   // parts of the three cuts of the table
+    Part* d_norm = nullptr;
+    Part* d_step = nullptr;                        // cut on whole lines of the flat buffers
+    Part* d_coded = nullptr;                       // cut on the layers' blocks
+    int32_t* d_begin = nullptr;                    // [L + 1] first of each layer's norm parts
+    double* d_partials = nullptr;                  // [n_norm]
+    StepFactors* d_factors = nullptr;
+    char error[256] = "";
+};
+
+namespace {
+
+int hip_fail(lgreco_optim* o, hipError_t e, const char* what) {
+    std::snprintf(o->error, sizeof(o->error), "%s: %s", what, hipGetErrorString(e));
+    return LGRECO_EHIP;
+}
+#define HIPCHK(expr)                                             \
+    do {                                                         \
+        hipError_t _e = (expr);                                  \
+        if (_e != hipSuccess) return hip_fail(o, _e, #expr);     \
+    } while (0)
+
+// The parts of one layer: `part` elements each, the first one cut short so that the others start at a multiple of `line` elements
+// of the flat buffers (1: at multiples of `part` from the layer's start).
+void cut_layer(std::vector<Part>& out, const lgreco_layer_t& a, int32_t l, int64_t block, float lr_scale, float decay_scale,
+               int64_t part, int64_t line) {
+    for (int64_t pos = 0; pos < a.numel;) {
+        const int64_t start = a.offset + pos;
+        const int64_t n = std::min(a.numel - pos, part - start % line);
+        out.push_back(Part{start, block + pos / kOptimBlock, (int32_t)n, (int32_t)pos, l, lr_scale, decay_scale, 0});
+        pos += n;
+    }
+}
+
+template <typename T>
+hipError_t to_device(T** d, const std::vector<T>& h) {
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(d), sizeof(T) * h.size());
+    return e != hipSuccess ? e : hipMemcpy(*d, h.data(), sizeof(T) * h.size(), hipMemcpyHostToDevice);
+}
+
+int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float* lr_scale, const float* decay_scale) {
+    const int st = check_layers(layers, L);
+    if (st != LGRECO_OK) return st;
+    std::vector<Part> norm, step, coded;
+    std::vector<int32_t> begin;
+    for (int32_t l = 0; l < L; ++l) {
+        const float ls = lr_scale ? lr_scale[l] : 1.0f, ds = decay_scale ? decay_scale[l] : 1.0f;
+        if (!(ls >= 0.0f && ls <= FLT_MAX) || !(ds >= 0.0f && ds <= FLT_MAX)) return LGRECO_EINVAL;
+        if (layers[l].offset > ((int64_t)1 << 58)) return LGRECO_EINVAL;     // (in bytes, beyond any address)
+        begin.push_back((int32_t)norm.size());
+        cut_layer(norm, layers[l], l, 0, ls, ds, kNormPart, kLine);
+        cut_layer(step, layers[l], l, 0, ls, ds, kStepPart, kLine);
+        cut_layer(coded, layers[l], l, o->blocks, ls, ds, kStepPart, 1);
+        o->blocks += (layers[l].numel + kOptimBlock - 1) / kOptimBlock;
+        if (step.size() > (size_t)1 << 23 || coded.size() > (size_t)1 << 23) return LGRECO_ENOSPACE;
+    }
+    begin.push_back((int32_t)norm.size());
+    o->L = L;
+    o->n_norm = (int64_t)norm.size();
+    o->n_step = (int64_t)step.size();
+    o->n_coded = (int64_t)coded.size();
+    HIPCHK(hipGetDevice(&o->device));
+    HIPCHK(to_device(&o->d_norm, norm));
+    HIPCHK(to_device(&o->d_step, step));
+    HIPCHK(to_device(&o->d_coded, coded));
+    HIPCHK(to_device(&o->d_begin, begin));
+    HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_partials), sizeof(double) * norm.size()));
+    HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_factors), sizeof(StepFactors)));
+    return LGRECO_OK;
+}
+
+int on_device(lgreco_optim* o) {
+    int d = -1;
+    HIPCHK(hipGetDevice(&d));
+    return d == o->device ? LGRECO_OK : LGRECO_EINVAL;
+}
+
+bool valid(const lgreco_adamw_t* c) {
+    const auto finite_from = [](double x, double least) { return x >= least && x <= DBL_MAX; };
+    return finite_from(c->lr, 0.0) && c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0 &&
+           c->eps <= FLT_MAX && (float)c->eps > 0.0f && finite_from(c->weight_decay, 0.0) && c->grad_scale > 0.0 &&
+           c->grad_scale <= DBL_MAX && finite_from(c->max_norm, 0.0) && (c->stochastic == 0 || c->stochastic == 1) && c->reserved == 0;
+}
+
+// What both forms of the step check and queue in front of their kernel.
+int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int32_t grad_type, float* params, const void* m,
+               const void* v, size_t moment_size, const void* copy, int32_t copy_type, const double* sumsq, const float* lr,
+               int64_t* step, hipStream_t s, StepParams* k) {
+    if (!o || !c || !grads || !params || !m || !v || !step || !valid(c)) return LGRECO_EINVAL;
+    if (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16) return LGRECO_EINVAL;
+    if (copy && copy_type != LGRECO_BF16 && copy_type != LGRECO_F16) return LGRECO_EINVAL;
+    if (c->max_norm > 0.0 && !sumsq) return LGRECO_EINVAL;
+    if (misaligned(grads, element_size(grad_type)) || misaligned(params, 4) || misaligned(m, moment_size) ||
+        misaligned(v, moment_size) || misaligned(copy, 2) || misaligned(sumsq, 8) || misaligned(lr, 4) || misaligned(step, 8))
+        return LGRECO_EINVAL;
+    const int st = on_device(o);
+    if (st != LGRECO_OK) return st;
+    *k = StepParams{nullptr, o->d_factors, grads, params, const_cast<void*>(m), const_cast<void*>(v), nullptr, const_cast<void*>(copy),
+                    c->weight_decay, (float)c->beta1, (float)(1.0 - c->beta1), (float)c->beta2, (float)(1.0 - c->beta2),
+                    (float)c->eps, c->stochastic, (uint32_t)c->seed, (uint32_t)(c->seed >> 32)};
+    const FactorParams fp{c->lr, c->beta1, c->beta2, c->grad_scale, c->max_norm, sumsq ? sumsq + o->L : nullptr, lr, step, o->d_factors};
+    HIPCHK(launch(factors_kernel, 1, 64, s, fp));
+    return LGRECO_OK;
+}
+
+typedef void (*StepKernel)(StepParams);
+
+template <typename G>
+StepKernel adamw_kernel_of(bool copy, int32_t copy_type) {
+    return !copy ? adamw_kernel<G, NoCopy> : copy_type == LGRECO_BF16 ? adamw_kernel<G, BF16> : adamw_kernel<G, F16>;
+}
+template <typename G, bool STOCHASTIC>
+StepKernel coded_kernel_of(bool copy, int32_t copy_type) {
+    return !copy ? adamw_coded_kernel<G, NoCopy, STOCHASTIC>
+                 : copy_type == LGRECO_BF16 ? adamw_coded_kernel<G, BF16, STOCHASTIC> : adamw_coded_kernel<G, F16, STOCHASTIC>;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int32_t L, const float* lr_scale,
+                        const float* decay_scale) {
+    if (!out) return LGRECO_EINVAL;
+    *out = nullptr;
+    lgreco_optim* o = new (std::nothrow) lgreco_optim();
+    if (!o) return LGRECO_ENOSPACE;
+    int st;
+    try {
+        st = create(o, layers, L, lr_scale, decay_scale);
+    } catch (...) {                                          // (host memory)
+        st = LGRECO_ENOSPACE;
+    }
+    if (st == LGRECO_OK) *out = o;
+    else lgreco_optim_destroy(o);
+    return st;
+}
+
+int lgreco_optim_destroy(lgreco_optim_t* o) {
+    if (!o) return LGRECO_EINVAL;
+    (void)hipFree(o->d_norm);
+    (void)hipFree(o->d_step);
+    (void)hipFree(o->d_coded);
+    (void)hipFree(o->d_begin);
+    (void)hipFree(o->d_partials);
+    (void)hipFree(o->d_factors);
+    delete o;
+    return LGRECO_OK;
+}
+
+int64_t lgreco_optim_blocks(const lgreco_optim_t* o) { return o ? o->blocks : -1; }
+
+const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o) { return o ? o->error : ""; }
+
+int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type, double* d_sumsq, void* stream) {
+    if (!o || !d_grads || !d_sumsq || (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16)) return LGRECO_EINVAL;
+    if (misaligned(d_grads, element_size(grad_type)) || misaligned(d_sumsq, 8)) return LGRECO_EINVAL;
+    const int st = on_device(o);
+    if (st != LGRECO_OK) return st;
+    hipStream_t s = (hipStream_t)stream;
+    const Part* const parts = o->d_norm;
+    if (grad_type == LGRECO_F32)
+        HIPCHK(launch(norm_part_kernel<float>, o->n_norm, kThreads, s, parts, static_cast<const float*>(d_grads), o->d_partials));
+    else
+        HIPCHK(launch(norm_part_kernel<BF16>, o->n_norm, kThreads, s, parts, static_cast<const BF16*>(d_grads), o->d_partials));
+    HIPCHK(launch(norm_layer_kernel, o->L, kThreads, s, (const double*)o->d_partials, (const int32_t*)o->d_begin, d_sumsq));
+    HIPCHK(launch(norm_total_kernel, 1, kThreads, s, d_sumsq, (int)o->L));
+    return LGRECO_OK;
+}
+
+int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
+                       float* d_params, float* d_m, float* d_v, void* d_copy, int32_t copy_type,
+                       const double* d_sumsq, const float* d_lr, int64_t* d_step, void* stream) {
+    hipStream_t s = (hipStream_t)stream;
+    StepParams k;
+    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 4, d_copy, copy_type, d_sumsq, d_lr, d_step, s, &k);
+    if (st != LGRECO_OK) return st;
+    k.parts = o->d_step;
+    const StepKernel f = grad_type == LGRECO_F32 ? adamw_kernel_of<float>(d_copy, copy_type) : adamw_kernel_of<BF16>(d_copy, copy_type);
+    HIPCHK(launch(f, o->n_step, kThreads, s, k));
+    return LGRECO_OK;
+}
+
+int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
+                             float* d_params, uint8_t* d_m, uint8_t* d_v, uint8_t* d_exps, void* d_copy,
+                             int32_t copy_type, const double* d_sumsq, const float* d_lr, int64_t* d_step,
+                             void* stream) {
+    hipStream_t s = (hipStream_t)stream;
+    if (!d_exps) return LGRECO_EINVAL;
+    StepParams k;
+    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 1, d_copy, copy_type, d_sumsq, d_lr, d_step, s, &k);
+    if (st != LGRECO_OK) return st;
+    k.parts = o->d_coded;
+    k.exps = d_exps;
+    StepKernel f;
+    if (cfg->stochastic)
+        f = grad_type == LGRECO_F32 ? coded_kernel_of<float, true>(d_copy, copy_type) : coded_kernel_of<BF16, true>(d_copy, copy_type);
+    else
+        f = grad_type == LGRECO_F32 ? coded_kernel_of<float, false>(d_copy, copy_type) : coded_kernel_of<BF16, false>(d_copy, copy_type);
+    HIPCHK(launch(f, o->n_coded, kThreads, s, k));
+    return LGRECO_OK;
+}
+
+int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_v, const uint8_t* d_exps,
+                        void* d_m_out, void* d_v_out, int32_t type, void* stream) {
+    if (!o || !d_m || !d_v || !d_exps || !d_m_out || !d_v_out || (type != LGRECO_F32 && type != LGRECO_BF16)) return LGRECO_EINVAL;
+    if (misaligned(d_m_out, element_size(type)) || misaligned(d_v_out, element_size(type))) return LGRECO_EINVAL;
+    const int st = on_device(o);
+    if (st != LGRECO_OK) return st;
+    hipStream_t s = (hipStream_t)stream;
+    const Part* const parts = o->d_coded;
+    if (type == LGRECO_F32)
+        HIPCHK(launch(moments_kernel<float>, o->n_coded, kThreads, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
+                      static_cast<float*>(d_v_out)));
+    else
+        HIPCHK(launch(moments_kernel<BF16>, o->n_coded, kThreads, s, parts, d_m, d_v, d_exps, static_cast<BF16*>(d_m_out),
+                      static_cast<BF16*>(d_v_out)));
+    return LGRECO_OK;
+}
+
+}  // extern "C"

@@ -6,6 +6,9 @@ the per-layer parameters, and the communication engine uses them until the next 
 
 This class only sequences calls of the C ABI (accumulate, profile_solve, payload_layout,
 compress); it does no arithmetic on gradients itself.
+
+AdamW is the other end of a step: the workers' payloads are turned back and summed, their sum's norm is
+taken, and the parameters are updated, again as calls of the C ABI alone.
 """
 from __future__ import annotations
 
@@ -54,3 +57,50 @@ class PeriodicRun:
             return None
         self.h.compress(d_grads, d_ef, self.layers, self.cands, self.choice, d_payload, self.offsets, d_q)
         return self.choice, self.offsets
+
+
+class AdamW:
+    """Parameters' update behind the exchange: moments (fp32, or 8 bits with `coded`), step count and norms of the
+    layers of one flat parameter buffer.  `layers` are all the tensors to be stepped, also those that travel
+    uncompressed.  With `guard` (always with clipping) a step whose gradients are not finite is left out.
+    Nothing waits for the GPU in `step`; it may be captured into a HIP graph."""
+
+    def __init__(self, layers, d_params, settings: "B.AdamW", lr_scale=None, decay_scale=None, coded: bool = False,
+                 d_copy=None, guard: bool = False):
+        import torch
+        self.plan = B.Optim(layers, lr_scale, decay_scale)
+        self.settings, self.d_params, self.d_copy, self.coded = settings, d_params, d_copy, coded
+        kind = torch.uint8 if coded else torch.float32
+        self.d_m, self.d_v = (torch.zeros(d_params.numel(), dtype=kind, device=d_params.device) for _ in range(2))
+        self.d_exps = torch.zeros(2 * self.plan.blocks, dtype=torch.uint8, device=d_params.device) if coded else None
+        self.d_step = torch.zeros(1, dtype=torch.int64, device=d_params.device)
+        self.d_sumsq = None
+        if guard or settings.max_norm > 0:
+            self.d_sumsq = torch.zeros(len(layers) + 1, dtype=torch.float64, device=d_params.device)
+
+    def step(self, d_grads, d_lr=None, stream=None):
+        """Norms, where they are wanted, and the update."""
+        if self.d_sumsq is not None:
+            self.plan.norms(d_grads, self.d_sumsq, stream=stream)
+        if self.coded:
+            self.plan.adamw_coded(self.settings, d_grads, self.d_params, self.d_m, self.d_v, self.d_exps, self.d_step,
+                                  d_copy=self.d_copy, d_sumsq=self.d_sumsq, d_lr=d_lr, stream=stream)
+        else:
+            self.plan.adamw(self.settings, d_grads, self.d_params, self.d_m, self.d_v, self.d_step, d_copy=self.d_copy,
+                            d_sumsq=self.d_sumsq, d_lr=d_lr, stream=stream)
+
+    def receive(self, handle: "B.Handle", d_payloads, offsets, layers, cands, choice, d_grads, d_lr=None, stream=None):
+        """The sum of the workers' payloads into d_grads, then a step on it (settings.grad_scale = 1 / workers makes
+        it the mean).  Layers that travel uncompressed hold their summed gradients in d_grads already."""
+        for w, payload in enumerate(d_payloads):
+            handle.decompress(payload, offsets, layers, cands, choice, d_grads, accumulate=w > 0, stream=stream)
+        self.step(d_grads, d_lr=d_lr, stream=stream)
+
+    def moments(self, stream=None):
+        """The moments as fp32 tensors (elements outside the layers: zero)."""
+        if not self.coded:
+            return self.d_m.clone(), self.d_v.clone()
+        import torch
+        out = [torch.zeros(self.d_m.numel(), dtype=torch.float32, device=self.d_m.device) for _ in range(2)]
+        self.plan.decode(self.d_m, self.d_v, self.d_exps, *out, stream=stream)
+        return tuple(out)
