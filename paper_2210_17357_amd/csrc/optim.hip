@@ -46,6 +46,7 @@ struct StepFactors {
 };
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 struct BF16 { uint16_t bits; };
@@ -70,6 +71,30 @@ __device__ __forceinline__ void store4(C* p, const float4 v) {
 }
 __device__ __forceinline__ void store4(float* p, const float4 v) { store_stream(p, v); }
 __device__ __forceinline__ void store4(NoCopy*, const float4) {}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const float4 a = load4(p), b = load4(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const BF16* p, float (&x)[8]) {
+    const u32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __builtin_bit_cast(float, v[j] << 16);
+        x[2 * j + 1] = __builtin_bit_cast(float, v[j] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    store_stream(p, make_float4(x[0], x[1], x[2], x[3]));
+    store_stream(p + 4, make_float4(x[4], x[5], x[6], x[7]));
+}
+template <typename C>
+__device__ __forceinline__ void store8(C* p, const float (&x)[8]) {
+    u32x4_any n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n[j] = (uint32_t)narrow_bits(x[2 * j], C{}) | (uint32_t)narrow_bits(x[2 * j + 1], C{}) << 16;
+    __builtin_nontemporal_store(n, reinterpret_cast<u32x4_any*>(p));
+}
+__device__ __forceinline__ void store8(NoCopy*, const float (&)[8]) {}
 template <typename C>
 __device__ __forceinline__ void store1(C* p, float v) { p->bits = narrow_bits(v, C{}); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
@@ -352,17 +377,41 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     }
 }
 
+// The values of 8 codes (two words of four bytes).
+__device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t (&cv)[2], int xm, int xv, float (&m)[8], float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        m[j] = decoded_m(cm[j >> 2] >> 8 * (j & 3) & 255u, xm);
+        v[j] = decoded_v(cv[j >> 2] >> 8 * (j & 3) & 255u, xv);
+    }
+}
+
+// Bound by HBM.  A thread takes 8 consecutive elements, all of one block.
 template <typename O>
 __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
                                                            O* __restrict__ m_out, O* __restrict__ v_out) {
     const Part t = parts[blockIdx.x];
-    const uint8_t* const m = codes_m + t.start;
-    const uint8_t* const v = codes_v + t.start;
-    const uint8_t* const x = exps + 2 * t.block;
-    for (int i = threadIdx.x; i < t.count; i += kThreads) {
-        store1(m_out + t.start + i, decoded_m(m[i], x[2 * (i / kOptimBlock)]));
-        store1(v_out + t.start + i, decoded_v(v[i], x[2 * (i / kOptimBlock) + 1]));
+    const int i = 8 * threadIdx.x, left = t.count - i;
+    if (left <= 0) return;
+    const uint8_t* const m = codes_m + t.start + i;
+    const uint8_t* const v = codes_v + t.start + i;
+    const uint8_t* const x = exps + 2 * (t.block + i / kOptimBlock);
+    O* const mo = m_out + t.start + i;
+    O* const vo = v_out + t.start + i;
+    const int xm = x[0], xv = x[1];
+    if (left >= 8) {
+        const u32x2_any a = *reinterpret_cast<const u32x2_any*>(m), b = *reinterpret_cast<const u32x2_any*>(v);
+        const uint32_t cm[2] = {a.x, a.y}, cv[2] = {b.x, b.y};
+        float fm[8], fv[8];
+        decode8(cm, cv, xm, xv, fm, fv);
+        store8(mo, fm);
+        store8(vo, fv);
+    } else {
+        for (int j = 0; j < left; ++j) {
+            store1(mo + j, decoded_m(m[j], xm));
+            store1(vo + j, decoded_v(v[j], xv));
+        }
     }
 }
 
