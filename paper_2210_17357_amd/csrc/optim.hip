@@ -46,8 +46,7 @@ struct StepFactors {
 };
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
 
 struct BF16 { uint16_t bits; };
 struct F16 { uint16_t bits; };
@@ -71,37 +70,36 @@ __device__ __forceinline__ void store4(C* p, const float4 v) {
 }
 __device__ __forceinline__ void store4(float* p, const float4 v) { store_stream(p, v); }
 __device__ __forceinline__ void store4(NoCopy*, const float4) {}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const float4 a = load4(p), b = load4(p + 4);
+template <typename C>
+__device__ __forceinline__ C* shifted(C* p, int64_t n) { return p + n; }
+__device__ __forceinline__ NoCopy* shifted(NoCopy* p, int64_t) { return p; }
+
+// The 8 elements of a block that one lane of a row of 16 takes: 4 from 4 * lane on and 4 from 64 + 4 * lane on, so that
+// every access of a row is whole lines.
+constexpr int kHalf = kOptimBlock / 2;
+__device__ __forceinline__ int place(int j) { return j < 4 ? j : kHalf - 4 + j; }
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+    const float4 a = load4(p), b = load4(p + kHalf);
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
 }
-__device__ __forceinline__ void load8(const BF16* p, float (&x)[8]) {
-    const u32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __builtin_bit_cast(float, v[j] << 16);
-        x[2 * j + 1] = __builtin_bit_cast(float, v[j] & 0xFFFF0000u);
-    }
+__device__ __forceinline__ void load8(const uint8_t* p, uint32_t (&c)[2]) {
+    c[0] = *reinterpret_cast<const u32_any*>(p);
+    c[1] = *reinterpret_cast<const u32_any*>(p + kHalf);
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    store_stream(p, make_float4(x[0], x[1], x[2], x[3]));
-    store_stream(p + 4, make_float4(x[4], x[5], x[6], x[7]));
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+    store4(p, make_float4(x[0], x[1], x[2], x[3]));
+    store4(shifted(p, kHalf), make_float4(x[4], x[5], x[6], x[7]));
 }
-template <typename C>
-__device__ __forceinline__ void store8(C* p, const float (&x)[8]) {
-    u32x4_any n;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) n[j] = (uint32_t)narrow_bits(x[2 * j], C{}) | (uint32_t)narrow_bits(x[2 * j + 1], C{}) << 16;
-    __builtin_nontemporal_store(n, reinterpret_cast<u32x4_any*>(p));
+__device__ __forceinline__ void store8(uint8_t* p, const uint32_t (&c)[2]) {
+    *reinterpret_cast<u32_any*>(p) = c[0];
+    *reinterpret_cast<u32_any*>(p + kHalf) = c[1];
 }
-__device__ __forceinline__ void store8(NoCopy*, const float (&)[8]) {}
 template <typename C>
 __device__ __forceinline__ void store1(C* p, float v) { p->bits = narrow_bits(v, C{}); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(NoCopy*, float) {}
-template <typename C>
-__device__ __forceinline__ C* shifted(C* p, int64_t n) { return p + n; }
-__device__ __forceinline__ NoCopy* shifted(NoCopy* p, int64_t) { return p; }
 
 // ------------------------------------------------------------------ norms
 template <typename G>
@@ -206,11 +204,13 @@ __device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams
     return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v};
 }
 
+// The root and the reciprocal are the instructions' (one unit in the last place), which take 8 cycles where the correctly
+// rounded ones take some 50.  (A v below 2^-126 may count as 0 in the denominator; eps is a normal number.)
 __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, float grad, float& p, float& m, float& v) {
     const float g = r.grad * grad;
     m = __builtin_fmaf(k.beta1, m, k.rest1 * g);
     v = __builtin_fmaf(k.beta2, v, k.rest2 * (g * g));
-    const float u = m / __builtin_fmaf(sqrtf(v), r.root_v, k.eps);
+    const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), r.root_v, k.eps));
     p -= __builtin_fmaf(r.shrink, p, r.rate * u);
 }
 
@@ -266,31 +266,44 @@ __device__ __forceinline__ float decoded_v(uint32_t code, int x) {
 // mantissa could carry into the next octave.
 __device__ __forceinline__ int block_exponent(uint32_t bits) { return (int)((bits + ((1u << kCodeShift) - 1)) >> 23); }
 
-// r: 16 random bits.
+// A magnitude on its way to a code: the code is bits 19.. of the sum, up to 7 or 8 of them.  r: 16 random bits from bit 3 on.  (A
+// number that is not finite leaves the field; its own byte alone takes what comes.)
 template <bool STOCHASTIC>
 __device__ __forceinline__ uint32_t encoded(float a, int shift, uint32_t r) {
     const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_ldexpf(a, shift));
-    const uint32_t add = STOCHASTIC ? (r << 3 | 4u) : ((1u << (kCodeShift - 1)) - 1) + (b >> kCodeShift & 1u);
-    return (b + add) >> kCodeShift;
+    return b + (STOCHASTIC ? ((r & 0x7FFF8u) | 4u) : ((1u << (kCodeShift - 1)) - 1) + (b >> kCodeShift & 1u));
 }
 
-__device__ __forceinline__ uint32_t row16_umax(uint32_t v) {
-    v = max(v, dpp_u32<kDppQuadXor1>(v));
-    v = max(v, dpp_u32<kDppQuadXor2>(v));
-    v = max(v, dpp_u32<kDppRowHalfMirror>(v));
-    v = max(v, dpp_u32<kDppRowMirror>(v));
-    return v;
+// Byte 3 of four words as one word.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0703u), __builtin_amdgcn_perm(b, a, 0x0C0C0703u), 0x05040100u);
 }
 
-// A thread takes 8 consecutive elements and a row of 16 lanes a block, so that the block's maxima take four vector
-// instructions each and no LDS.
+// max(|a|, |b|, c): magnitudes of results of arithmetic
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, |%1|, |%2|, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// The values of 8 codes (two words of four bytes).
+__device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t (&cv)[2], int xm, int xv, float (&m)[8], float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        m[j] = decoded_m(cm[j >> 2] >> 8 * (j & 3) & 255u, xm);
+        v[j] = decoded_v(cv[j >> 2] >> 8 * (j & 3) & 255u, xv);
+    }
+}
+
+// A row of 16 lanes takes a block, so that its maxima take four vector instructions each and no LDS.
 template <typename G, typename C, bool STOCHASTIC>
 __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     const StepFactors f = *k.factors;
     if (!f.go) return;
     const Part t = k.parts[blockIdx.x];
     const Rates r = rates_of(f, k, t);
-    const int i = 8 * threadIdx.x, left = t.count - i;
+    const int lane = threadIdx.x & 15, i = threadIdx.x / 16 * kOptimBlock + 4 * lane, left = t.count - i;
+    const bool whole = i - 4 * lane + kOptimBlock <= t.count;
     const G* const g = static_cast<const G*>(k.grads) + t.start + i;
     float* const p = k.p + t.start + i;
     uint8_t* const m = static_cast<uint8_t*>(k.m) + t.start + i;
@@ -305,94 +318,80 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
         xm = exps[0];
         xv = exps[1];
     }
-    if (left >= 8) {
-        const float4 ga = load4(g), gb = load4(g + 4), pa = load4(p), pb = load4(p + 4);
-        const u32x2_any a = *reinterpret_cast<const u32x2_any*>(m), b = *reinterpret_cast<const u32x2_any*>(v);
-        cm[0] = a.x; cm[1] = a.y; cv[0] = b.x; cv[1] = b.y;
-        gi[0] = ga.x; gi[1] = ga.y; gi[2] = ga.z; gi[3] = ga.w; gi[4] = gb.x; gi[5] = gb.y; gi[6] = gb.z; gi[7] = gb.w;
-        pi[0] = pa.x; pi[1] = pa.y; pi[2] = pa.z; pi[3] = pa.w; pi[4] = pb.x; pi[5] = pb.y; pi[6] = pb.z; pi[7] = pb.w;
+    if (whole) {
+        load8(g, gi);
+        load8(p, pi);
+        load8(m, cm);
+        load8(v, cv);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool in = j < left;
-            gi[j] = in ? widen(g[j]) : 0.0f;
-            pi[j] = in ? p[j] : 0.0f;
-            cm[j >> 2] |= in ? (uint32_t)m[j] << 8 * (j & 3) : 0u;
-            cv[j >> 2] |= in ? (uint32_t)v[j] << 8 * (j & 3) : 0u;
+            const bool in = place(j) < left;
+            gi[j] = in ? widen(g[place(j)]) : 0.0f;
+            pi[j] = in ? p[place(j)] : 0.0f;
+            cm[j >> 2] |= in ? (uint32_t)m[place(j)] << 8 * (j & 3) : 0u;
+            cv[j >> 2] |= in ? (uint32_t)v[place(j)] << 8 * (j & 3) : 0u;
         }
     }
     // (elements past the layer's end: gradient 0 and codes 0, so their moments are 0)
-    uint32_t top_m = 0, top_v = 0;
+    decode8(cm, cv, xm, xv, mi, vi);
+    float top_m = 0.0f, top_v = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        mi[j] = decoded_m(cm[j >> 2] >> 8 * (j & 3) & 255u, xm);
-        vi[j] = decoded_v(cv[j >> 2] >> 8 * (j & 3) & 255u, xv);
-        step_one(k, r, gi[j], pi[j], mi[j], vi[j]);
-        top_m = max(top_m, __builtin_bit_cast(uint32_t, mi[j]) & 0x7FFFFFFFu);
-        top_v = max(top_v, __builtin_bit_cast(uint32_t, vi[j]));
-    }
-    xm = min(block_exponent(row16_umax(top_m)), 255);
-    xv = min(block_exponent(row16_umax(top_v)), 255);
-    Philox4 words[2] = {};
-    if (STOCHASTIC) {
-        const uint32_t quad = (uint32_t)(t.pos + i) / 4;
-        words[0] = philox4x32_10(quad, f.t_lo, (uint32_t)t.layer, 1u + f.t_hi, k.seed_lo, k.seed_hi);
-        words[1] = philox4x32_10(quad + 1, f.t_lo, (uint32_t)t.layer, 1u + f.t_hi, k.seed_lo, k.seed_hi);
-    }
-    cm[0] = cm[1] = cv[0] = cv[1] = 0;
+    for (int j = 0; j < 8; ++j) step_one(k, r, gi[j], pi[j], mi[j], vi[j]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t w = words[j >> 2].w[j & 3];
-        const uint32_t sign = __builtin_bit_cast(uint32_t, mi[j]) >> 31 << 7;
-        const uint32_t a = min(encoded<STOCHASTIC>(__builtin_fabsf(mi[j]), kTopM - xm, w & 0xFFFFu), 127u) | sign;
-        const uint32_t b = max(min(encoded<STOCHASTIC>(vi[j], kTopV - xv, w >> 16), 255u), vi[j] > 0.0f ? 1u : 0u);
-        cm[j >> 2] |= a << 8 * (j & 3);
-        cv[j >> 2] |= b << 8 * (j & 3);
+    for (int j = 0; j < 8; j += 2) {
+        top_m = max3_abs(mi[j], mi[j + 1], top_m);
+        top_v = max3f(vi[j], vi[j + 1], top_v);
+    }
+    xm = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_m)));
+    xv = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_v)));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        Philox4 words{};
+        if (STOCHASTIC)
+            words = philox4x32_10((uint32_t)(t.pos + i) / 4 + h * (kHalf / 4), f.t_lo, (uint32_t)t.layer, 1u + f.t_hi, k.seed_lo, k.seed_hi);
+        uint32_t em[4], ev[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float mj = mi[4 * h + q], vj = vi[4 * h + q];
+            const uint32_t a = encoded<STOCHASTIC>(__builtin_fabsf(mj), kTopM - xm, words.w[q] << 3);
+            const uint32_t b = max(encoded<STOCHASTIC>(vj, kTopV - xv, words.w[q] >> 13), vj > 0.0f ? 1u << kCodeShift : 0u);
+            em[q] = (a << 5 & 0x7FFFFFFFu) | (__builtin_bit_cast(uint32_t, mj) & 0x80000000u);
+            ev[q] = b << 5;
+        }
+        cm[h] = top_bytes(em[0], em[1], em[2], em[3]);
+        cv[h] = top_bytes(ev[0], ev[1], ev[2], ev[3]);
     }
     if (left <= 0) return;
-    if ((threadIdx.x & 15) == 0) {
+    if (lane == 0) {
         exps[0] = (uint8_t)xm;
         exps[1] = (uint8_t)xv;
     }
-    if (left >= 8) {
-        u32x2_any a, b;
-        a.x = cm[0]; a.y = cm[1]; b.x = cv[0]; b.y = cv[1];
-        *reinterpret_cast<u32x2_any*>(m) = a;
-        *reinterpret_cast<u32x2_any*>(v) = b;
-        const float4 pa = make_float4(pi[0], pi[1], pi[2], pi[3]), pb = make_float4(pi[4], pi[5], pi[6], pi[7]);
-        store4(p, pa);
-        store4(p + 4, pb);
-        store4(copy, pa);
-        store4(shifted(copy, 4), pb);
+    if (whole) {
+        store8(m, cm);
+        store8(v, cv);
+        store8(p, pi);
+        store8(copy, pi);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (j < left) {
-                p[j] = pi[j];
-                m[j] = (uint8_t)(cm[j >> 2] >> 8 * (j & 3));
-                v[j] = (uint8_t)(cv[j >> 2] >> 8 * (j & 3));
-                store1(shifted(copy, j), pi[j]);
+            if (place(j) < left) {
+                p[place(j)] = pi[j];
+                m[place(j)] = (uint8_t)(cm[j >> 2] >> 8 * (j & 3));
+                v[place(j)] = (uint8_t)(cv[j >> 2] >> 8 * (j & 3));
+                store1(shifted(copy, place(j)), pi[j]);
             }
         }
     }
 }
 
-// The values of 8 codes (two words of four bytes).
-__device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t (&cv)[2], int xm, int xv, float (&m)[8], float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        m[j] = decoded_m(cm[j >> 2] >> 8 * (j & 3) & 255u, xm);
-        v[j] = decoded_v(cv[j >> 2] >> 8 * (j & 3) & 255u, xv);
-    }
-}
-
-// Bound by HBM.  A thread takes 8 consecutive elements, all of one block.
+// Bound by HBM.  A row of 16 lanes takes a block.
 template <typename O>
 __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
                                                            O* __restrict__ m_out, O* __restrict__ v_out) {
     const Part t = parts[blockIdx.x];
-    const int i = 8 * threadIdx.x, left = t.count - i;
+    const int lane = threadIdx.x & 15, i = threadIdx.x / 16 * kOptimBlock + 4 * lane, left = t.count - i;
     if (left <= 0) return;
     const uint8_t* const m = codes_m + t.start + i;
     const uint8_t* const v = codes_v + t.start + i;
@@ -400,17 +399,18 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restric
     O* const mo = m_out + t.start + i;
     O* const vo = v_out + t.start + i;
     const int xm = x[0], xv = x[1];
-    if (left >= 8) {
-        const u32x2_any a = *reinterpret_cast<const u32x2_any*>(m), b = *reinterpret_cast<const u32x2_any*>(v);
-        const uint32_t cm[2] = {a.x, a.y}, cv[2] = {b.x, b.y};
+    if (i - 4 * lane + kOptimBlock <= t.count) {
+        uint32_t cm[2], cv[2];
         float fm[8], fv[8];
+        load8(m, cm);
+        load8(v, cv);
         decode8(cm, cv, xm, xv, fm, fv);
         store8(mo, fm);
         store8(vo, fv);
     } else {
-        for (int j = 0; j < left; ++j) {
-            store1(mo + j, decoded_m(m[j], xm));
-            store1(vo + j, decoded_v(v[j], xv));
+        for (int j = 0; j < 8 && place(j) < left; ++j) {
+            store1(mo + place(j), decoded_m(m[place(j)], xm));
+            store1(vo + place(j), decoded_v(v[place(j)], xv));
         }
     }
 }
@@ -514,7 +514,7 @@ int on_device(lgreco_optim* o) {
 bool valid(const lgreco_adamw_t* c) {
     const auto finite_from = [](double x, double least) { return x >= least && x <= DBL_MAX; };
     return finite_from(c->lr, 0.0) && c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0 &&
-           c->eps <= FLT_MAX && (float)c->eps > 0.0f && finite_from(c->weight_decay, 0.0) && c->grad_scale > 0.0 &&
+           c->eps <= FLT_MAX && (float)c->eps >= FLT_MIN && finite_from(c->weight_decay, 0.0) && c->grad_scale > 0.0 &&
            c->grad_scale <= DBL_MAX && finite_from(c->max_norm, 0.0) && (c->stochastic == 0 || c->stochastic == 1) && c->reserved == 0;
 }
 
