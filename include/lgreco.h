@@ -425,8 +425,8 @@ typedef struct {
     int32_t  reserved;      /* must be 0 */
 } lgreco_adamw_t;
 
-/* Creates a plan for these layers on the current device (48 bytes for every 1024 elements of device memory,
- * or less).
+/* Creates a plan for these layers on the current device.  It takes about 64 bytes of device memory for every 1024 elements
+ * and 130 for every layer; tables of more than 2^24 - 1 pieces of 1024 elements (17 G elements): LGRECO_ENOSPACE.
  *   lr_scale     host [L] factors of lr per layer, or NULL (= 1): finite, >= 0
  *   decay_scale  host [L] factors of weight_decay per layer, or NULL (= 1): finite, >= 0 */
 int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int32_t L, const float* lr_scale,

@@ -18,8 +18,10 @@ namespace lgreco {
 namespace {
 
 constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
-constexpr int kNormPart = 16384;     // elements of a workgroup of the norms
-constexpr int kStepPart = 2048;      // elements of a workgroup of the step
+constexpr int kNormPart = 16384;     // elements of a workgroup of the norms (four times that where they are many)
+constexpr int kStepPart = 4 * kThreads;        // elements of a workgroup of the step: one access a thread and buffer
+constexpr int kCodedPart = 8 * kThreads;       // the same with 8-bit moments
+constexpr int64_t kMaxParts = ((int64_t)1 << 32) / kThreads - 1;   // (a launch takes fewer than 2^32 threads)
 constexpr int kLine = 32;            // elements of a 128-byte line of fp32
 
 // What one workgroup works on: consecutive elements of one layer.
@@ -214,38 +216,40 @@ __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, fl
     p -= __builtin_fmaf(r.shrink, p, r.rate * u);
 }
 
+// Bound by HBM, four streams in and three or four out.  A thread takes 4 elements and is done: 355 M elements in 1725 us
+// (28 bytes each: 5.8 TB/s), 1810 with two rounds a workgroup, 1870 with eight; 1955 without the streaming hints.
 template <typename G, typename C>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
     const StepFactors f = *k.factors;
     if (!f.go) return;
     const Part t = k.parts[blockIdx.x];
     const Rates r = rates_of(f, k, t);
-    const G* const g = static_cast<const G*>(k.grads) + t.start;
-    float* const p = k.p + t.start;
-    float* const m = static_cast<float*>(k.m) + t.start;
-    float* const v = static_cast<float*>(k.v) + t.start;
-    C* const copy = shifted(static_cast<C*>(k.copy), t.start);
-    const int tid = threadIdx.x;
-    for (int i = 4 * tid; i + 4 <= t.count; i += 4 * kThreads) {
-        const float4 gi = load4(g + i);
-        float4 pi = load4(p + i), mi = load4(m + i), vi = load4(v + i);
+    const int i = 4 * threadIdx.x, left = t.count - i;
+    const G* const g = static_cast<const G*>(k.grads) + t.start + i;
+    float* const p = k.p + t.start + i;
+    float* const m = static_cast<float*>(k.m) + t.start + i;
+    float* const v = static_cast<float*>(k.v) + t.start + i;
+    C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
+    if (left >= 4) {
+        const float4 gi = load4(g);
+        float4 pi = load4(p), mi = load4(m), vi = load4(v);
         step_one(k, r, gi.x, pi.x, mi.x, vi.x);
         step_one(k, r, gi.y, pi.y, mi.y, vi.y);
         step_one(k, r, gi.z, pi.z, mi.z, vi.z);
         step_one(k, r, gi.w, pi.w, mi.w, vi.w);
-        store4(p + i, pi);
-        store4(m + i, mi);
-        store4(v + i, vi);
-        store4(copy + (__is_same(C, NoCopy) ? 0 : i), pi);
-    }
-    if (tid < (t.count & 3)) {
-        const int i = (t.count & ~3) + tid;
-        float pi = p[i], mi = m[i], vi = v[i];
-        step_one(k, r, widen(g[i]), pi, mi, vi);
-        p[i] = pi;
-        m[i] = mi;
-        v[i] = vi;
-        store1(copy + (__is_same(C, NoCopy) ? 0 : i), pi);
+        store4(p, pi);
+        store4(m, mi);
+        store4(v, vi);
+        store4(copy, pi);
+    } else {
+        for (int j = 0; j < left; ++j) {
+            float pj = p[j], mj = m[j], vj = v[j];
+            step_one(k, r, widen(g[j]), pj, mj, vj);
+            p[j] = pj;
+            m[j] = mj;
+            v[j] = vj;
+            store1(shifted(copy, j), pj);
+        }
     }
 }
 
@@ -479,16 +483,19 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
     if (st != LGRECO_OK) return st;
     std::vector<Part> norm, step, coded;
     std::vector<int32_t> begin;
+    int64_t total = 0;
+    for (int32_t l = 0; l < L; ++l) total += layers[l].numel;
+    const int64_t norm_part = total / kNormPart <= 8192 ? kNormPart : 4 * kNormPart;
     for (int32_t l = 0; l < L; ++l) {
         const float ls = lr_scale ? lr_scale[l] : 1.0f, ds = decay_scale ? decay_scale[l] : 1.0f;
         if (!(ls >= 0.0f && ls <= FLT_MAX) || !(ds >= 0.0f && ds <= FLT_MAX)) return LGRECO_EINVAL;
         if (layers[l].offset > ((int64_t)1 << 58)) return LGRECO_EINVAL;     // (in bytes, beyond any address)
         begin.push_back((int32_t)norm.size());
-        cut_layer(norm, layers[l], l, 0, ls, ds, kNormPart, kLine);
+        cut_layer(norm, layers[l], l, 0, ls, ds, norm_part, kLine);
         cut_layer(step, layers[l], l, 0, ls, ds, kStepPart, kLine);
-        cut_layer(coded, layers[l], l, o->blocks, ls, ds, kStepPart, 1);
+        cut_layer(coded, layers[l], l, o->blocks, ls, ds, kCodedPart, 1);
         o->blocks += (layers[l].numel + kOptimBlock - 1) / kOptimBlock;
-        if (step.size() > (size_t)1 << 23 || coded.size() > (size_t)1 << 23) return LGRECO_ENOSPACE;
+        if ((int64_t)step.size() > kMaxParts) return LGRECO_ENOSPACE;       // (the finest of the cuts)
     }
     begin.push_back((int32_t)norm.size());
     o->L = L;
