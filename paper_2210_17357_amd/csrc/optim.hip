@@ -44,8 +44,9 @@ struct StepFactors {
     float root_v;        // 1 / sqrt(1 - b2^t)
     uint32_t t_lo, t_hi; // t
     int32_t go;          // 0: the step is left out
-    int32_t pad[3];
+    int32_t pad;
 };
+constexpr int kFactorWords = sizeof(StepFactors) / 4;
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
@@ -103,6 +104,29 @@ __device__ __forceinline__ void store1(C* p, float v) { p->bits = narrow_bits(v,
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(NoCopy*, float) {}
 
+// ------------------------------------------------------------------ the last workgroup
+// Whether the caller's workgroup is the last of its launch (one thread asks, once): tickets of 32 workgroups each, then one of
+// the groups, so that no word of memory takes more than 64 of them.  The last ones clear the words for the next launch.
+//   ORDERED: what the other workgroups wrote before is visible to the last one
+constexpr int kTicketGroup = 32;
+constexpr int kTicketParts = 2048;       // most workgroups of such a launch
+constexpr int kTicketLine = 32;          // words apart
+constexpr int kTicketWords = kTicketLine * (1 + kTicketParts / kTicketGroup);
+template <bool ORDERED>
+__device__ __forceinline__ uint32_t draw(uint32_t* word) {
+    return __hip_atomic_fetch_add(word, 1u, ORDERED ? __ATOMIC_ACQ_REL : __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool ORDERED>
+__device__ __forceinline__ bool last_workgroup(uint32_t* tickets) {
+    const uint32_t n = gridDim.x, group = blockIdx.x / kTicketGroup, groups = (n + kTicketGroup - 1) / kTicketGroup;
+    uint32_t* const mine = tickets + kTicketLine * (1 + group);
+    if (draw<ORDERED>(mine) != min((uint32_t)kTicketGroup, n - group * kTicketGroup) - 1) return false;
+    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (draw<ORDERED>(tickets) != groups - 1) return false;
+    __hip_atomic_store(tickets, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
 // ------------------------------------------------------------------ norms
 template <typename G>
 __global__ __launch_bounds__(kThreads) void norm_part_kernel(const Part* __restrict__ parts, const G* __restrict__ grads,
@@ -155,11 +179,9 @@ struct FactorParams {
     const double* total;     // sum of the squared gradients, or null
     const float* lr_factor;  // or null
     int64_t* step;
-    StepFactors* out;
 };
 
-__global__ __launch_bounds__(64) void factors_kernel(FactorParams p) {
-    if (threadIdx.x != 0) return;
+__device__ __forceinline__ StepFactors factors_of(const FactorParams& p) {
     StepFactors f{};
     double c = p.grad_scale;
     f.go = 1;
@@ -168,21 +190,39 @@ __global__ __launch_bounds__(64) void factors_kernel(FactorParams p) {
         if (!(s <= DBL_MAX)) f.go = 0;                           // NaN or infinite
         if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * sqrt(s) + 1e-6));
     }
-    const int64_t t = *p.step + 1;
+    const uint64_t t = (uint64_t)(*p.step + 1);
+    // b^t by squaring: its relative error is some t 2^-53, and b^t is 0 long before that matters
+    double power1 = 1.0, power2 = 1.0, b1 = p.beta1, b2 = p.beta2;
+    for (uint64_t n = t; n; n >>= 1) {
+        if (n & 1) {
+            power1 *= b1;
+            power2 *= b2;
+        }
+        b1 *= b1;
+        b2 *= b2;
+    }
     f.lr = p.lr_factor ? p.lr * (double)*p.lr_factor : p.lr;
-    f.lr_m = f.lr / (1.0 - pow(p.beta1, (double)t));
-    f.root_v = (float)(1.0 / sqrt(1.0 - pow(p.beta2, (double)t)));
+    f.lr_m = f.lr / (1.0 - power1);
+    f.root_v = (float)(1.0 / sqrt(1.0 - power2));
     f.grad = (float)c;
     f.t_lo = (uint32_t)t;
-    f.t_hi = (uint32_t)((uint64_t)t >> 32);
-    *p.out = f;
-    if (f.go) *p.step = t;
+    f.t_hi = (uint32_t)(t >> 32);
+    return f;
+}
+
+__global__ __launch_bounds__(64) void factors_kernel(FactorParams p, StepFactors* out) {
+    if (threadIdx.x != 0) return;
+    const StepFactors f = factors_of(p);
+    *out = f;
+    if (f.go) *p.step = (int64_t)((uint64_t)f.t_hi << 32 | f.t_lo);
 }
 
 // ------------------------------------------------------------------ AdamW
 struct StepParams {
     const Part* parts;
-    const StepFactors* factors;
+    const StepFactors* factors;    // null: the workgroups work them out themselves
+    FactorParams raw;
+    uint32_t* tickets;
     const void* grads;
     float* p;
     void* m;
@@ -194,6 +234,33 @@ struct StepParams {
     int32_t stochastic;
     uint32_t seed_lo, seed_hi;
 };
+
+// The step's factors: from the kernel in front, or, where the table is short and a kernel in front would take as long as the
+// step, worked out by every workgroup's first wavefront while its data is on the way.  Then the last workgroup to finish
+// counts the step: every other one has read the count by then, with its first wavefront, which also draws its ticket.
+__device__ __forceinline__ StepFactors step_factors(const StepParams& k) {
+    if (k.factors) return *k.factors;
+    __shared__ uint32_t s_words[kFactorWords];
+    if (threadIdx.x < 64) {
+        const StepFactors f = factors_of(k.raw);
+        uint32_t w[kFactorWords];
+        __builtin_memcpy(w, &f, sizeof(f));
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < kFactorWords; ++i) s_words[i] = w[i];
+        }
+    }
+    __syncthreads();
+    uint32_t w[kFactorWords];
+#pragma unroll
+    for (int i = 0; i < kFactorWords; ++i) w[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_words[i]);
+    StepFactors f;
+    __builtin_memcpy(&f, w, sizeof(f));
+    return f;
+}
+__device__ __forceinline__ void count_step(const StepParams& k, const StepFactors& f) {
+    if (!k.factors && threadIdx.x == 0 && last_workgroup<false>(k.tickets)) *k.raw.step = (int64_t)((uint64_t)f.t_hi << 32 | f.t_lo);
+}
 
 // The factors of one layer's elements.
 struct Rates {
@@ -220,19 +287,24 @@ __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, fl
 // (28 bytes each: 5.8 TB/s), 1810 with two rounds a workgroup, 1870 with eight; 1955 without the streaming hints.
 template <typename G, typename C>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
-    const StepFactors f = *k.factors;
-    if (!f.go) return;
     const Part t = k.parts[blockIdx.x];
-    const Rates r = rates_of(f, k, t);
     const int i = 4 * threadIdx.x, left = t.count - i;
     const G* const g = static_cast<const G*>(k.grads) + t.start + i;
     float* const p = k.p + t.start + i;
     float* const m = static_cast<float*>(k.m) + t.start + i;
     float* const v = static_cast<float*>(k.v) + t.start + i;
     C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
+    float4 gi{}, pi{}, mi{}, vi{};
     if (left >= 4) {
-        const float4 gi = load4(g);
-        float4 pi = load4(p), mi = load4(m), vi = load4(v);
+        gi = load4(g);
+        pi = load4(p);
+        mi = load4(m);
+        vi = load4(v);
+    }
+    const StepFactors f = step_factors(k);
+    if (!f.go) return;
+    const Rates r = rates_of(f, k, t);
+    if (left >= 4) {
         step_one(k, r, gi.x, pi.x, mi.x, vi.x);
         step_one(k, r, gi.y, pi.y, mi.y, vi.y);
         step_one(k, r, gi.z, pi.z, mi.z, vi.z);
@@ -251,6 +323,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
             store1(shifted(copy, j), pj);
         }
     }
+    count_step(k, f);
 }
 
 // ------------------------------------------------------------------ 8-bit moments
@@ -302,10 +375,7 @@ __device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t 
 // A row of 16 lanes takes a block, so that its maxima take four vector instructions each and no LDS.
 template <typename G, typename C, bool STOCHASTIC>
 __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
-    const StepFactors f = *k.factors;
-    if (!f.go) return;
     const Part t = k.parts[blockIdx.x];
-    const Rates r = rates_of(f, k, t);
     const int lane = threadIdx.x & 15, i = threadIdx.x / 16 * kOptimBlock + 4 * lane, left = t.count - i;
     const bool whole = i - 4 * lane + kOptimBlock <= t.count;
     const G* const g = static_cast<const G*>(k.grads) + t.start + i;
@@ -337,6 +407,9 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
             cv[j >> 2] |= in ? (uint32_t)v[place(j)] << 8 * (j & 3) : 0u;
         }
     }
+    const StepFactors f = step_factors(k);
+    if (!f.go) return;
+    const Rates r = rates_of(f, k, t);
     // (elements past the layer's end: gradient 0 and codes 0, so their moments are 0)
     decode8(cm, cv, xm, xv, mi, vi);
     float top_m = 0.0f, top_v = 0.0f;
@@ -387,6 +460,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
             }
         }
     }
+    count_step(k, f);                                        // (every workgroup's first thread has elements)
 }
 
 // Bound by HBM.  A row of 16 lanes takes a block.
@@ -445,6 +519,7 @@ struct lgreco_optim {
     int32_t* d_begin = nullptr;                    // [L + 1] first of each layer's norm parts
     double* d_partials = nullptr;                  // [n_norm]
     StepFactors* d_factors = nullptr;
+    uint32_t* d_tickets = nullptr;                 // zero between launches
     char error[256] = "";
 };
 
@@ -509,6 +584,7 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
     HIPCHK(to_device(&o->d_begin, begin));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_partials), sizeof(double) * norm.size()));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_factors), sizeof(StepFactors)));
+    HIPCHK(to_device(&o->d_tickets, std::vector<uint32_t>(kTicketWords, 0u)));
     return LGRECO_OK;
 }
 
@@ -528,8 +604,8 @@ bool valid(const lgreco_adamw_t* c) {
 // What both forms of the step check and queue in front of their kernel.
 int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int32_t grad_type, float* params, const void* m,
                const void* v, size_t moment_size, const void* copy, int32_t copy_type, const double* sumsq, const float* lr,
-               int64_t* step, hipStream_t s, StepParams* k) {
-    if (!o || !c || !grads || !params || !m || !v || !step || !valid(c)) return LGRECO_EINVAL;
+               int64_t* step, hipStream_t s, const Part* parts, int64_t n_parts, StepParams* k) {
+    if (!c || !grads || !params || !m || !v || !step || !valid(c)) return LGRECO_EINVAL;
     if (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16) return LGRECO_EINVAL;
     if (copy && copy_type != LGRECO_BF16 && copy_type != LGRECO_F16) return LGRECO_EINVAL;
     if (c->max_norm > 0.0 && !sumsq) return LGRECO_EINVAL;
@@ -538,11 +614,12 @@ int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int3
         return LGRECO_EINVAL;
     const int st = on_device(o);
     if (st != LGRECO_OK) return st;
-    *k = StepParams{nullptr, o->d_factors, grads, params, const_cast<void*>(m), const_cast<void*>(v), nullptr, const_cast<void*>(copy),
-                    c->weight_decay, (float)c->beta1, (float)(1.0 - c->beta1), (float)c->beta2, (float)(1.0 - c->beta2),
-                    (float)c->eps, c->stochastic, (uint32_t)c->seed, (uint32_t)(c->seed >> 32)};
-    const FactorParams fp{c->lr, c->beta1, c->beta2, c->grad_scale, c->max_norm, sumsq ? sumsq + o->L : nullptr, lr, step, o->d_factors};
-    HIPCHK(launch(factors_kernel, 1, 64, s, fp));
+    const FactorParams raw{c->lr, c->beta1, c->beta2, c->grad_scale, c->max_norm, sumsq ? sumsq + o->L : nullptr, lr, step};
+    const bool short_table = n_parts <= kTicketParts;
+    *k = StepParams{parts, short_table ? nullptr : o->d_factors, raw, o->d_tickets, grads, params, const_cast<void*>(m),
+                    const_cast<void*>(v), nullptr, const_cast<void*>(copy), c->weight_decay, (float)c->beta1, (float)(1.0 - c->beta1),
+                    (float)c->beta2, (float)(1.0 - c->beta2), (float)c->eps, c->stochastic, (uint32_t)c->seed, (uint32_t)(c->seed >> 32)};
+    if (!short_table) HIPCHK(launch(factors_kernel, 1, 64, s, raw, o->d_factors));
     return LGRECO_OK;
 }
 
@@ -587,6 +664,7 @@ int lgreco_optim_destroy(lgreco_optim_t* o) {
     (void)hipFree(o->d_begin);
     (void)hipFree(o->d_partials);
     (void)hipFree(o->d_factors);
+    (void)hipFree(o->d_tickets);
     delete o;
     return LGRECO_OK;
 }
@@ -615,10 +693,10 @@ int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void*
                        float* d_params, float* d_m, float* d_v, void* d_copy, int32_t copy_type,
                        const double* d_sumsq, const float* d_lr, int64_t* d_step, void* stream) {
     hipStream_t s = (hipStream_t)stream;
+    if (!o) return LGRECO_EINVAL;
     StepParams k;
-    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 4, d_copy, copy_type, d_sumsq, d_lr, d_step, s, &k);
+    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 4, d_copy, copy_type, d_sumsq, d_lr, d_step, s, o->d_step, o->n_step, &k);
     if (st != LGRECO_OK) return st;
-    k.parts = o->d_step;
     const StepKernel f = grad_type == LGRECO_F32 ? adamw_kernel_of<float>(d_copy, copy_type) : adamw_kernel_of<BF16>(d_copy, copy_type);
     HIPCHK(launch(f, o->n_step, kThreads, s, k));
     return LGRECO_OK;
@@ -629,11 +707,10 @@ int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const
                              int32_t copy_type, const double* d_sumsq, const float* d_lr, int64_t* d_step,
                              void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    if (!d_exps) return LGRECO_EINVAL;
+    if (!o || !d_exps) return LGRECO_EINVAL;
     StepParams k;
-    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 1, d_copy, copy_type, d_sumsq, d_lr, d_step, s, &k);
+    const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 1, d_copy, copy_type, d_sumsq, d_lr, d_step, s, o->d_coded, o->n_coded, &k);
     if (st != LGRECO_OK) return st;
-    k.parts = o->d_coded;
     k.exps = d_exps;
     StepKernel f;
     if (cfg->stochastic)
