@@ -18,13 +18,26 @@ namespace lgreco {
 namespace {
 
 constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
-constexpr int kNormPart = 16384;     // elements of a workgroup of the norms (four times that where they are many)
+// Elements of a workgroup of the norms, doubled while there would be more than kNormParts: enough workgroups to fill the chip
+// more than once, few enough partial sums (355 M elements, us: 16384 a workgroup 215, 65536 213, 131072 212, 262144 232; of bf16 133, 138,
+// 164; 67 M of bf16: 38, 49, 75 and 130, with 32768 36; 25 M: 22, 24, 30, 47).
+constexpr int kNormPart = 16384, kNormParts = 6000;
 constexpr int kStepPart = 4 * kThreads;        // elements of a workgroup of the step: one access a thread and buffer
 constexpr int kCodedPart = 8 * kThreads;       // the same with 8-bit moments
+constexpr int kShortParts = 16384;          // most workgroups of a step that works out its own factors
 constexpr int64_t kMaxParts = ((int64_t)1 << 32) / kThreads - 1;   // (a launch takes fewer than 2^32 threads)
 constexpr int kLine = 32;            // elements of a 128-byte line of fp32
 
-// What one workgroup works on: consecutive elements of one layer.
+// What one workgroup of the norms adds up: consecutive elements of one layer, its layer's part `index` of `parts`.
+struct NormPart {
+    int64_t start;
+    int32_t count, layer;
+    int32_t index, parts;
+    int32_t ticket;      // the layer's first ticket word, where it has more parts than one
+    int32_t pad;
+};
+
+// What one workgroup of the step works on: consecutive elements of one layer.
 struct Part {
     int64_t start;       // first element, into the flat buffers
     int64_t block;       // 8-bit moments: its first block
@@ -49,6 +62,7 @@ struct StepFactors {
 constexpr int kFactorWords = sizeof(StepFactors) / 4;
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
 struct BF16 { uint16_t bits; };
@@ -64,6 +78,19 @@ __device__ __forceinline__ float4 load4(const float* p) { return load_stream(p);
 __device__ __forceinline__ float4 load4(const BF16* p) {
     const u16x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
     return make_float4(widen(BF16{v.x}), widen(BF16{v.y}), widen(BF16{v.z}), widen(BF16{v.w}));
+}
+// one 16-byte access
+__device__ __forceinline__ void load16(const float* p, float (&x)[4]) {
+    const float4 v = load_stream(p);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+__device__ __forceinline__ void load16(const BF16* p, float (&x)[8]) {
+    const u32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __builtin_bit_cast(float, v[j] << 16);
+        x[2 * j + 1] = __builtin_bit_cast(float, v[j] & 0xFFFF0000u);
+    }
 }
 template <typename C>
 __device__ __forceinline__ void store4(C* p, const float4 v) {
@@ -105,73 +132,102 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(NoCopy*, float) {}
 
 // ------------------------------------------------------------------ the last workgroup
-// Whether the caller's workgroup is the last of its launch (one thread asks, once): tickets of 32 workgroups each, then one of
-// the groups, so that no word of memory takes more than 64 of them.  The last ones clear the words for the next launch.
-//   ORDERED: what the other workgroups wrote before is visible to the last one
-constexpr int kTicketGroup = 32;
-constexpr int kTicketParts = 2048;       // most workgroups of such a launch
-constexpr int kTicketLine = 32;          // words apart
-constexpr int kTicketWords = kTicketLine * (1 + kTicketParts / kTicketGroup);
-template <bool ORDERED>
-__device__ __forceinline__ uint32_t draw(uint32_t* word) {
-    return __hip_atomic_fetch_add(word, 1u, ORDERED ? __ATOMIC_ACQ_REL : __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Whether the caller is the last of n that ask, the i-th one: a ticket among 64 neighbours, then one of their groups, so that no
+// word of memory takes more than 64 of them (one word for 4000 workgroups: 30 us where these take 12).  The last ones clear the words for the next launch.  (Of more than 64 * 64,
+// groups are larger.)
+// Tickets order nothing by themselves: an ordered one writes back and drops the L2 caches, which took the norms of 355 M
+// elements from 212 to 360 us.  What the last one reads is published by an exchange, which is performed where all caches
+// meet before it returns, and read by loads of the same scope.
+constexpr int kTicketGroup = 64;
+constexpr int kTicketLine = 32;                                // words apart
+constexpr int kTicketWords = kTicketLine * (1 + kTicketGroup);
+__host__ __device__ inline uint32_t ticket_group(uint32_t n) {
+    return n > kTicketGroup * kTicketGroup ? (n + kTicketGroup - 1) / kTicketGroup : kTicketGroup;
 }
-template <bool ORDERED>
-__device__ __forceinline__ bool last_workgroup(uint32_t* tickets) {
-    const uint32_t n = gridDim.x, group = blockIdx.x / kTicketGroup, groups = (n + kTicketGroup - 1) / kTicketGroup;
-    uint32_t* const mine = tickets + kTicketLine * (1 + group);
-    if (draw<ORDERED>(mine) != min((uint32_t)kTicketGroup, n - group * kTicketGroup) - 1) return false;
-    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (draw<ORDERED>(tickets) != groups - 1) return false;
-    __hip_atomic_store(tickets, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__host__ __device__ inline uint32_t ticket_lines(uint32_t n) { return n <= kTicketGroup ? 1 : 1 + (n + ticket_group(n) - 1) / ticket_group(n); }
+__device__ __forceinline__ bool last_drawn(uint32_t* word, uint32_t n) {
+    if (__hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != n - 1) return false;
+    __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return true;
+}
+__device__ __forceinline__ bool last_of(uint32_t* tickets, uint32_t i, uint32_t n) {
+    if (n <= kTicketGroup) return last_drawn(tickets, n);
+    const uint32_t size = ticket_group(n), group = i / size, groups = (n + size - 1) / size;
+    return last_drawn(tickets + kTicketLine * (1 + group), min(size, n - group * size)) && last_drawn(tickets, groups);
+}
+__device__ __forceinline__ void publish(double* p, double x) {
+    uint64_t old = __hip_atomic_exchange(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" : "+v"(old) : : "memory");               // (it has returned before anything that follows)
+}
+__device__ __forceinline__ double published(const double* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // ------------------------------------------------------------------ norms
-template <typename G>
-__global__ __launch_bounds__(kThreads) void norm_part_kernel(const Part* __restrict__ parts, const G* __restrict__ grads,
-                                                             double* __restrict__ partials) {
-    __shared__ double s_sum[kThreads / 64];
-    const Part t = parts[blockIdx.x];
-    const G* const g = grads + t.start;
-    const int tid = threadIdx.x;
-    double a0 = 0.0, a1 = 0.0, a2 = 0.0, a3 = 0.0;
-#pragma unroll 4
-    for (int i = 4 * tid; i + 4 <= t.count; i += 4 * kThreads) {
-        const float4 x = load4(g + i);
-        a0 = __builtin_fma((double)x.x, (double)x.x, a0);
-        a1 = __builtin_fma((double)x.y, (double)x.y, a1);
-        a2 = __builtin_fma((double)x.z, (double)x.z, a2);
-        a3 = __builtin_fma((double)x.w, (double)x.w, a3);
-    }
-    if (tid < (t.count & 3)) {
-        const double x = (double)widen(g[(t.count & ~3) + tid]);
-        a0 = __builtin_fma(x, x, a0);
-    }
-    const double w = wave_sum((a0 + a1) + (a2 + a3));
-    if ((tid & 63) == 0) s_sum[tid >> 6] = w;
-    __syncthreads();
-    if (tid == 0) partials[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-}
+struct NormParams {
+    const NormPart* parts;
+    const void* grads;
+    double* partials;
+    double* sumsq;             // [L + 1]
+    int32_t L;
+    uint32_t* tickets;         // of the layers; then the layers' own, of their parts
+};
 
-// Sum of n doubles in an order that depends on n alone, one workgroup.
-__device__ __forceinline__ void sum_block(const double* __restrict__ x, int n, double* out) {
-    __shared__ double s_sum[kThreads / 64];
-    const int tid = threadIdx.x;
-    double a = 0.0;
-    for (int i = tid; i < n; i += kThreads) a += x[i];
+__device__ __forceinline__ double sum_of_waves(double a, double* s_sum) {
     const double w = wave_sum(a);
-    if ((tid & 63) == 0) s_sum[tid >> 6] = w;
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = w;
     __syncthreads();
-    if (tid == 0) *out = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    return (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+// Sum of n published numbers in an order that depends on n alone.
+__device__ __forceinline__ double sum_published(const double* p, int n, double* s_sum) {
+    double a = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kThreads) a += published(p + i);
+    return sum_of_waves(a, s_sum);
 }
 
-__global__ __launch_bounds__(kThreads) void norm_layer_kernel(const double* __restrict__ partials, const int32_t* __restrict__ begin,
-                                                              double* __restrict__ sumsq) {
-    const int b = begin[blockIdx.x];
-    sum_block(partials + b, begin[blockIdx.x + 1] - b, sumsq + blockIdx.x);
+// Bound by HBM.  The last workgroup of a layer adds up the layer's partial sums, the last of those the layers' sums.
+template <typename G>
+__global__ __launch_bounds__(kThreads) void norms_kernel(NormParams k) {
+    __shared__ double s_sum[3][kThreads / 64];
+    __shared__ int s_last[2];
+    const NormPart t = k.parts[blockIdx.x];
+    const G* const g = static_cast<const G*>(k.grads) + t.start;
+    const int tid = threadIdx.x;
+    constexpr int kWide = 16 / sizeof(G);
+    double a[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
+    for (int i = kWide * tid; i + kWide <= t.count; i += kWide * kThreads) {
+        float x[kWide];
+        load16(g + i, x);
+#pragma unroll
+        for (int j = 0; j < kWide; ++j) a[j & 3] = __builtin_fma((double)x[j], (double)x[j], a[j & 3]);
+    }
+    if (tid < t.count % kWide) {
+        const double x = (double)widen(g[t.count / kWide * kWide + tid]);
+        a[0] = __builtin_fma(x, x, a[0]);
+    }
+    double sum = sum_of_waves((a[0] + a[1]) + (a[2] + a[3]), s_sum[0]);
+    if (t.parts > 1) {
+        if (tid == 0) {
+            publish(k.partials + blockIdx.x, sum);
+            s_last[0] = last_of(k.tickets + t.ticket, t.index, t.parts);
+        }
+        __syncthreads();
+        if (!s_last[0]) return;
+        sum = sum_published(k.partials + (blockIdx.x - t.index), t.parts, s_sum[1]);
+    }
+    if (tid == 0) {
+        publish(k.sumsq + t.layer, sum);
+        s_last[1] = last_of(k.tickets, t.layer, k.L);
+    }
+    __syncthreads();
+    if (!s_last[1]) return;
+    sum = sum_published(k.sumsq, k.L, s_sum[2]);
+    if (tid == 0) k.sumsq[k.L] = sum;
 }
-__global__ __launch_bounds__(kThreads) void norm_total_kernel(double* __restrict__ sumsq, int n) { sum_block(sumsq, n, sumsq + n); }
 
 // ------------------------------------------------------------------ the step's factors
 struct FactorParams {
@@ -259,7 +315,7 @@ __device__ __forceinline__ StepFactors step_factors(const StepParams& k) {
     return f;
 }
 __device__ __forceinline__ void count_step(const StepParams& k, const StepFactors& f) {
-    if (!k.factors && threadIdx.x == 0 && last_workgroup<false>(k.tickets)) *k.raw.step = (int64_t)((uint64_t)f.t_hi << 32 | f.t_lo);
+    if (!k.factors && threadIdx.x == 0 && last_of(k.tickets, blockIdx.x, gridDim.x)) *k.raw.step = (int64_t)((uint64_t)f.t_hi << 32 | f.t_lo);
 }
 
 // The factors of one layer's elements.
@@ -513,13 +569,13 @@ struct lgreco_optim {
     int32_t L = 0;
     int64_t blocks = 0;
     int64_t n_norm = 0, n_step = 0, n_coded = 0;   // parts of the three cuts of the table
-    Part* d_norm = nullptr;
+    NormPart* d_norm = nullptr;
     Part* d_step = nullptr;                        // cut on whole lines of the flat buffers
     Part* d_coded = nullptr;                       // cut on the layers' blocks
-    int32_t* d_begin = nullptr;                    // [L + 1] first of each layer's norm parts
     double* d_partials = nullptr;                  // [n_norm]
     StepFactors* d_factors = nullptr;
-    uint32_t* d_tickets = nullptr;                 // zero between launches
+    uint32_t* d_tickets = nullptr;                 // of the step; zero between launches, like
+    uint32_t* d_norm_tickets = nullptr;            // those of the norms
     char error[256] = "";
 };
 
@@ -535,14 +591,13 @@ int hip_fail(lgreco_optim* o, hipError_t e, const char* what) {
         if (_e != hipSuccess) return hip_fail(o, _e, #expr);     \
     } while (0)
 
-// The parts of one layer: `part` elements each, the first one cut short so that the others start at a multiple of `line` elements
-// of the flat buffers (1: at multiples of `part` from the layer's start).
-void cut_layer(std::vector<Part>& out, const lgreco_layer_t& a, int32_t l, int64_t block, float lr_scale, float decay_scale,
-               int64_t part, int64_t line) {
+// Calls f(first element, the same from the layer's start, elements) for the parts of one layer: `part` elements each, the first one
+// cut short so that the others start at a multiple of `line` elements of the flat buffers (1: wherever the layer starts).
+template <typename F>
+void for_parts(const lgreco_layer_t& a, int64_t part, int64_t line, F f) {
     for (int64_t pos = 0; pos < a.numel;) {
-        const int64_t start = a.offset + pos;
-        const int64_t n = std::min(a.numel - pos, part - start % line);
-        out.push_back(Part{start, block + pos / kOptimBlock, (int32_t)n, (int32_t)pos, l, lr_scale, decay_scale, 0});
+        const int64_t start = a.offset + pos, n = std::min(a.numel - pos, part - start % line);
+        f(start, pos, n);
         pos += n;
     }
 }
@@ -556,23 +611,33 @@ hipError_t to_device(T** d, const std::vector<T>& h) {
 int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float* lr_scale, const float* decay_scale) {
     const int st = check_layers(layers, L);
     if (st != LGRECO_OK) return st;
-    std::vector<Part> norm, step, coded;
-    std::vector<int32_t> begin;
+    std::vector<NormPart> norm;
+    std::vector<Part> step, coded;
+    size_t norm_tickets = (size_t)kTicketLine * ticket_lines((uint32_t)L);
     int64_t total = 0;
     for (int32_t l = 0; l < L; ++l) total += layers[l].numel;
-    const int64_t norm_part = total / kNormPart <= 8192 ? kNormPart : 4 * kNormPart;
+    int64_t norm_part = kNormPart;
+    while (total / norm_part > kNormParts) norm_part *= 2;
     for (int32_t l = 0; l < L; ++l) {
         const float ls = lr_scale ? lr_scale[l] : 1.0f, ds = decay_scale ? decay_scale[l] : 1.0f;
         if (!(ls >= 0.0f && ls <= FLT_MAX) || !(ds >= 0.0f && ds <= FLT_MAX)) return LGRECO_EINVAL;
         if (layers[l].offset > ((int64_t)1 << 58)) return LGRECO_EINVAL;     // (in bytes, beyond any address)
-        begin.push_back((int32_t)norm.size());
-        cut_layer(norm, layers[l], l, 0, ls, ds, norm_part, kLine);
-        cut_layer(step, layers[l], l, 0, ls, ds, kStepPart, kLine);
-        cut_layer(coded, layers[l], l, o->blocks, ls, ds, kCodedPart, 1);
+        const size_t first = norm.size();
+        for_parts(layers[l], norm_part, kLine, [&](int64_t start, int64_t, int64_t n) {
+            norm.push_back(NormPart{start, (int32_t)n, l, (int32_t)(norm.size() - first), 0, (int32_t)norm_tickets, 0});
+        });
+        const size_t parts = norm.size() - first;
+        for (size_t i = first; i < norm.size(); ++i) norm[i].parts = (int32_t)parts;
+        if (parts > 1) norm_tickets += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
+        for_parts(layers[l], kStepPart, kLine, [&](int64_t start, int64_t pos, int64_t n) {
+            step.push_back(Part{start, 0, (int32_t)n, (int32_t)pos, l, ls, ds, 0});
+        });
+        for_parts(layers[l], kCodedPart, 1, [&](int64_t start, int64_t pos, int64_t n) {
+            coded.push_back(Part{start, o->blocks + pos / kOptimBlock, (int32_t)n, (int32_t)pos, l, ls, ds, 0});
+        });
         o->blocks += (layers[l].numel + kOptimBlock - 1) / kOptimBlock;
         if ((int64_t)step.size() > kMaxParts) return LGRECO_ENOSPACE;       // (the finest of the cuts)
     }
-    begin.push_back((int32_t)norm.size());
     o->L = L;
     o->n_norm = (int64_t)norm.size();
     o->n_step = (int64_t)step.size();
@@ -581,10 +646,10 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
     HIPCHK(to_device(&o->d_norm, norm));
     HIPCHK(to_device(&o->d_step, step));
     HIPCHK(to_device(&o->d_coded, coded));
-    HIPCHK(to_device(&o->d_begin, begin));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_partials), sizeof(double) * norm.size()));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_factors), sizeof(StepFactors)));
     HIPCHK(to_device(&o->d_tickets, std::vector<uint32_t>(kTicketWords, 0u)));
+    HIPCHK(to_device(&o->d_norm_tickets, std::vector<uint32_t>(norm_tickets, 0u)));
     return LGRECO_OK;
 }
 
@@ -615,7 +680,7 @@ int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int3
     const int st = on_device(o);
     if (st != LGRECO_OK) return st;
     const FactorParams raw{c->lr, c->beta1, c->beta2, c->grad_scale, c->max_norm, sumsq ? sumsq + o->L : nullptr, lr, step};
-    const bool short_table = n_parts <= kTicketParts;
+    const bool short_table = n_parts <= kShortParts;
     *k = StepParams{parts, short_table ? nullptr : o->d_factors, raw, o->d_tickets, grads, params, const_cast<void*>(m),
                     const_cast<void*>(v), nullptr, const_cast<void*>(copy), c->weight_decay, (float)c->beta1, (float)(1.0 - c->beta1),
                     (float)c->beta2, (float)(1.0 - c->beta2), (float)c->eps, c->stochastic, (uint32_t)c->seed, (uint32_t)(c->seed >> 32)};
@@ -661,10 +726,10 @@ int lgreco_optim_destroy(lgreco_optim_t* o) {
     (void)hipFree(o->d_norm);
     (void)hipFree(o->d_step);
     (void)hipFree(o->d_coded);
-    (void)hipFree(o->d_begin);
     (void)hipFree(o->d_partials);
     (void)hipFree(o->d_factors);
     (void)hipFree(o->d_tickets);
+    (void)hipFree(o->d_norm_tickets);
     delete o;
     return LGRECO_OK;
 }
@@ -679,13 +744,8 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
     const int st = on_device(o);
     if (st != LGRECO_OK) return st;
     hipStream_t s = (hipStream_t)stream;
-    const Part* const parts = o->d_norm;
-    if (grad_type == LGRECO_F32)
-        HIPCHK(launch(norm_part_kernel<float>, o->n_norm, kThreads, s, parts, static_cast<const float*>(d_grads), o->d_partials));
-    else
-        HIPCHK(launch(norm_part_kernel<BF16>, o->n_norm, kThreads, s, parts, static_cast<const BF16*>(d_grads), o->d_partials));
-    HIPCHK(launch(norm_layer_kernel, o->L, kThreads, s, (const double*)o->d_partials, (const int32_t*)o->d_begin, d_sumsq));
-    HIPCHK(launch(norm_total_kernel, 1, kThreads, s, d_sumsq, (int)o->L));
+    const NormParams k{o->d_norm, d_grads, o->d_partials, d_sumsq, o->L, o->d_norm_tickets};
+    HIPCHK(launch(grad_type == LGRECO_F32 ? norms_kernel<float> : norms_kernel<BF16>, o->n_norm, kThreads, s, k));
     return LGRECO_OK;
 }
 
