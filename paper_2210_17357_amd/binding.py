@@ -395,6 +395,7 @@ class Optim:
     def __init__(self, layers, lr_scale: Optional[Sequence[float]] = None, decay_scale: Optional[Sequence[float]] = None):
         import torch
         self._o = C.c_void_p()
+        self._current_stream = torch.cuda.current_stream
         scales = []
         for a in (lr_scale, decay_scale):
             a = None if a is None else np.ascontiguousarray(a, np.float32)
@@ -434,18 +435,21 @@ class Optim:
         """Device address of a tensor that has to be of this type (None: one of the floating types a call takes) and size."""
         if t is None:
             return None
-        if not t.is_cuda or not t.is_contiguous() or t.get_device() != self.device:
+        if t.get_device() != self.device or not t.is_contiguous():
             raise ValueError("expected a contiguous tensor on the plan's device")
-        if (t.dtype is not dtype) if dtype is not None else (t.dtype not in self._types):
+        if t.dtype is not dtype and (dtype is not None or t.dtype not in self._types):
             raise ValueError("unexpected tensor type %s" % t.dtype)
         if t.numel() < numel:
             raise ValueError("the tensor has %d elements, the layers reach to %d" % (t.numel(), numel))
         return t.data_ptr()
 
+    def _stream(self, stream) -> int:
+        return self._current_stream(self.device).cuda_stream if stream is None else int(stream)
+
     def norms(self, d_grads, d_sumsq, stream=None):
         """d_sumsq (fp64, layers + 1): squared norm of every layer's gradient, then of all together."""
         self._check(lib().lgreco_optim_norms(self._o, self._ptr(d_grads, None, self.extent), self._types[d_grads.dtype],
-                                             self._ptr(d_sumsq, self._f64, self.L + 1), _stream(stream)))
+                                             self._ptr(d_sumsq, self._f64, self.L + 1), self._stream(stream)))
 
     def adamw(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_step, d_copy=None, d_sumsq=None, d_lr=None, stream=None):
         """One step with fp32 moments; gradients fp32 or bf16, d_copy (bf16 or fp16) receives the parameters too."""
@@ -454,7 +458,7 @@ class Optim:
             self._o, C.byref(settings), self._ptr(d_grads, None, n), self._types[d_grads.dtype], self._ptr(d_params, self._f32, n),
             self._ptr(d_m, self._f32, n), self._ptr(d_v, self._f32, n), self._ptr(d_copy, None, n),
             0 if d_copy is None else self._types[d_copy.dtype], self._ptr(d_sumsq, self._f64, self.L + 1),
-            self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1), _stream(stream)))
+            self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1), self._stream(stream)))
 
     def adamw_coded(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_exps, d_step, d_copy=None, d_sumsq=None, d_lr=None,
                     stream=None):
@@ -465,7 +469,7 @@ class Optim:
             self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
             self._ptr(d_copy, None, n), 0 if d_copy is None else self._types[d_copy.dtype],
             self._ptr(d_sumsq, self._f64, self.L + 1), self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1),
-            _stream(stream)))
+            self._stream(stream)))
 
     def decode(self, d_m, d_v, d_exps, d_m_out, d_v_out, stream=None):
         """Values of 8-bit moments, both outputs fp32 or both bf16."""
@@ -474,4 +478,4 @@ class Optim:
             raise ValueError("outputs of one type")
         self._check(lib().lgreco_optim_decode(
             self._o, self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
-            self._ptr(d_m_out, None, n), self._ptr(d_v_out, None, n), self._types[d_m_out.dtype], _stream(stream)))
+            self._ptr(d_m_out, None, n), self._ptr(d_v_out, None, n), self._types[d_m_out.dtype], self._stream(stream)))

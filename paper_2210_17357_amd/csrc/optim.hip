@@ -63,6 +63,7 @@ constexpr int kFactorWords = sizeof(StepFactors) / 4;
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
 struct BF16 { uint16_t bits; };
@@ -91,6 +92,18 @@ __device__ __forceinline__ void load16(const BF16* p, float (&x)[8]) {
         x[2 * j] = __builtin_bit_cast(float, v[j] << 16);
         x[2 * j + 1] = __builtin_bit_cast(float, v[j] & 0xFFFF0000u);
     }
+}
+template <typename C>
+__device__ __forceinline__ void store16(C* p, const float (&x)[8]) {
+    u32x4_any n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n[j] = (uint32_t)narrow_bits(x[2 * j], C{}) | (uint32_t)narrow_bits(x[2 * j + 1], C{}) << 16;
+    __builtin_nontemporal_store(n, reinterpret_cast<u32x4_any*>(p));
+}
+__device__ __forceinline__ void load_run(const uint8_t* p, uint32_t (&c)[2]) {
+    const u32x2_any v = *reinterpret_cast<const u32x2_any*>(p);
+    c[0] = v.x;
+    c[1] = v.y;
 }
 template <typename C>
 __device__ __forceinline__ void store4(C* p, const float4 v) {
@@ -519,32 +532,47 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     count_step(k, f);                                        // (every workgroup's first thread has elements)
 }
 
-// Bound by HBM.  A row of 16 lanes takes a block.
+// Bound by HBM.  A row of 16 lanes takes a block; for 16-bit values a lane takes 8 consecutive elements, one access of each
+// buffer (355 M elements: 365 us, 5.8 TB/s, 390 as for fp32).
 template <typename O>
 __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
                                                            O* __restrict__ m_out, O* __restrict__ v_out) {
+    constexpr bool kRun = sizeof(O) == 2;
     const Part t = parts[blockIdx.x];
-    const int lane = threadIdx.x & 15, i = threadIdx.x / 16 * kOptimBlock + 4 * lane, left = t.count - i;
+    const int lane = threadIdx.x & 15, first = threadIdx.x / 16 * kOptimBlock;
+    const int i = first + (kRun ? 8 : 4) * lane, left = t.count - i;
     if (left <= 0) return;
     const uint8_t* const m = codes_m + t.start + i;
     const uint8_t* const v = codes_v + t.start + i;
-    const uint8_t* const x = exps + 2 * (t.block + i / kOptimBlock);
+    const uint8_t* const x = exps + 2 * (t.block + first / kOptimBlock);
     O* const mo = m_out + t.start + i;
     O* const vo = v_out + t.start + i;
     const int xm = x[0], xv = x[1];
-    if (i - 4 * lane + kOptimBlock <= t.count) {
+    if (first + kOptimBlock <= t.count) {
         uint32_t cm[2], cv[2];
         float fm[8], fv[8];
-        load8(m, cm);
-        load8(v, cv);
+        if constexpr (kRun) {
+            load_run(m, cm);
+            load_run(v, cv);
+        } else {
+            load8(m, cm);
+            load8(v, cv);
+        }
         decode8(cm, cv, xm, xv, fm, fv);
-        store8(mo, fm);
-        store8(vo, fv);
+        if constexpr (kRun) {
+            store16(mo, fm);
+            store16(vo, fv);
+        } else {
+            store8(mo, fm);
+            store8(vo, fv);
+        }
     } else {
-        for (int j = 0; j < 8 && place(j) < left; ++j) {
-            store1(mo + place(j), decoded_m(m[place(j)], xm));
-            store1(vo + place(j), decoded_v(v[place(j)], xv));
+        for (int j = 0; j < 8; ++j) {
+            const int at = kRun ? j : place(j);
+            if (at >= left) break;
+            store1(mo + at, decoded_m(m[at], xm));
+            store1(vo + at, decoded_v(v[at], xv));
         }
     }
 }
