@@ -447,7 +447,8 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
  * (c = grad_scale without clipping), lr_l = lr * *d_lr * lr_scale[l] and wd_l = weight_decay * decay_scale[l]:
  *   g = c * grad;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + (1 - beta2) g^2
  *   p' = p - lr_l wd_l p - lr_l / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
- * in fp32, the factors that are the same for all elements in fp64.
+ * in fp32, the factors that are the same for all elements in fp64.  Of m' and v' every factor, product and sum is
+ * rounded to fp32 (c as well), so that they are reproducible bit for bit: v' = beta2 * v + (1 - beta2) * (g * g).
  *   grad_type  LGRECO_F32 or LGRECO_BF16
  *   d_params   fp32, in/out;   d_m, d_v  fp32 moments, in/out (zero before the first step)
  *   d_copy     out: p' rounded to nearest even in copy_type (LGRECO_BF16 or LGRECO_F16; fp16: beyond

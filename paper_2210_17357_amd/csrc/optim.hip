@@ -342,12 +342,14 @@ __device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams
     return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v};
 }
 
+// The moments' products and sums are rounded one by one, so that they, and the codes made of them, are what any other fp32
+// program finds (a fused product moves one code in some ten million to its neighbour).
 // The root and the reciprocal are the instructions' (one unit in the last place), which take 8 cycles where the correctly
 // rounded ones take some 50.  (A v below 2^-126 may count as 0 in the denominator; eps is a normal number.)
 __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, float grad, float& p, float& m, float& v) {
     const float g = r.grad * grad;
-    m = __builtin_fmaf(k.beta1, m, k.rest1 * g);
-    v = __builtin_fmaf(k.beta2, v, k.rest2 * (g * g));
+    m = k.beta1 * m + k.rest1 * g;
+    v = k.beta2 * v + k.rest2 * (g * g);
     const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), r.root_v, k.eps));
     p -= __builtin_fmaf(r.shrink, p, r.rate * u);
 }
@@ -414,10 +416,16 @@ __device__ __forceinline__ int block_exponent(uint32_t bits) { return (int)((bit
 
 // A magnitude on its way to a code: the code is bits 19.. of the sum, up to 7 or 8 of them.  r: 16 random bits from bit 3 on.  (A
 // number that is not finite leaves the field; its own byte alone takes what comes.)
+// Below the lowest octave the scaled number is denormal and has been rounded: it is taken down again where that went up, and its
+// last bit set where anything was lost, so that ties are ties and the sum carries only where the exact one does.
+// (Random bits end above the last one, which they need not see.)
 template <bool STOCHASTIC>
 __device__ __forceinline__ uint32_t encoded(float a, int shift, uint32_t r) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_ldexpf(a, shift));
-    return b + (STOCHASTIC ? ((r & 0x7FFF8u) | 4u) : ((1u << (kCodeShift - 1)) - 1) + (b >> kCodeShift & 1u));
+    const float scaled = __builtin_ldexpf(a, shift), back = __builtin_ldexpf(scaled, -shift);
+    uint32_t b = __builtin_bit_cast(uint32_t, scaled) - (back > a ? 1u : 0u);
+    if (STOCHASTIC) return b + ((r & 0x7FFF8u) | 4u);
+    b |= back != a ? 1u : 0u;
+    return b + ((1u << (kCodeShift - 1)) - 1) + (b >> kCodeShift & 1u);
 }
 
 // Byte 3 of four words as one word.

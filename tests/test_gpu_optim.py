@@ -406,6 +406,40 @@ def test_coded_blocks_at_their_borders(stochastic):
     assert (gv[(np.abs(g) > 1e-15)] > 0).all()
 
 
+@pytest.mark.parametrize("stochastic", [False, True])
+def test_codes_of_moments_known_exactly(stochastic):
+    """With both betas 0, m' is the gradient and v' its square in fp32: every code and exponent has to be the definition's.  Ties
+    and the numbers beside them, in every octave and below the lowest one, and magnitudes of every size."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    rng = np.random.default_rng(15)
+    ties = np.concatenate([(np.arange(16) + 0.5) * 2.0 ** -10] + [(np.arange(16, 32) + 0.5) * 2.0 ** (e - 4) for e in range(-6, 0)])
+    beside = [ties, np.nextafter(ties.astype(np.float32), np.float32(0)), np.nextafter(ties.astype(np.float32), np.float32(1)),
+              ties * (1 + 2.0 ** -14), ties * (1 - 2.0 ** -14)]
+    blocks = [np.r_[1.0, b, np.zeros(127 - b.size)] for b in beside]
+    blocks += [2.0 ** rng.uniform(-24, 0, 128) * rng.choice([-1, 1], 128) for _ in range(400)]
+    roots = rng.integers(1, 2048, (100, 128)) * 2.0 ** -rng.integers(11, 21, (100, 128))      # squares of 11 bits: exact, ties among them
+    g = np.concatenate([np.concatenate(blocks), roots.reshape(-1)]).astype(np.float32)
+    n = g.size
+    plan = B.Optim(table(B, [0], [n]))
+    d = [torch.from_numpy(g).cuda(), torch.zeros(n, device="cuda")]
+    d += [torch.zeros(k, dtype=torch.uint8, device="cuda") for k in (n, n, 2 * plan.blocks)]
+    s = B.adamw(lr=1e-3, beta1=0.0, beta2=0.0, stochastic=stochastic, seed=6)
+    plan.adamw_coded(s, *d, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    gm, gv, gx = (a.cpu().numpy() for a in d[2:])
+    u = O.halves(6, 1, 0, n) if stochastic else (None, None)
+    for k, (a, codes, octaves, signed) in enumerate(((g, gm, O.OCTAVES_M, True), (g * g, gv, O.OCTAVES_V, False))):
+        got = stored(codes, gx.reshape(-1, 2)[:, k], octaves, signed)
+        for b in range(plan.blocks):
+            c = slice(128 * b, 128 * (b + 1))
+            x = O.exponent(np.abs(a[c]))
+            assert x == gx[2 * b + k]
+            want = O.rounded(np.abs(a[c]), x, octaves, u[k] if u[k] is None else u[k][c])
+            if not signed:
+                want = np.where(a[c] > 0, np.maximum(want, 2.0 ** (x - 127.0 - 14 - 4)), want)
+            assert np.array_equal(got[c], np.copysign(want, a[c]) if signed else want), (k, b)
+
+
 def test_stochastic_rounding_keeps_the_expectation():
     """v that falls by a thousandth a step: rounded to the nearest it stays, stochastically it falls as in 64 bits.
     65536 elements; a step's rounding has a variance of at most (v / 16)^2 / 4, so 400 of them and a mean over the
