@@ -491,6 +491,88 @@ def test_decode(name, kind):
     assert all((a[~inside] == 5.0).all() for a in got)
 
 
+# ------------------------------------------------------------------------------ long tables
+@pytest.mark.parametrize("coded", [False, True])
+def test_a_long_table_is_its_layers_one_by_one(coded):
+    """More workgroups than work out their own factors, layers of more than 64 parts: bit for bit what plans of one layer
+    each give."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    numels = np.array([40_000_003, 77, 2_500_001, 1])
+    offs = np.cumsum(numels + 1) - numels
+    n = int(offs[-1] + numels[-1]) + 2
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    g = torch.randn(n, generator=gen, device="cuda") * 1e-3
+    p = torch.randn(n, generator=gen, device="cuda")
+    plan = B.Optim(table(B, offs, numels), [1.0, 0.5, 2.0, 1.0], [1.0, 0.0, 1.0, 0.5])
+    s = B.adamw(lr=1e-3, max_norm=1.0, grad_scale=0.3, weight_decay=0.1)
+    sums = torch.zeros(5, dtype=torch.float64, device="cuda")
+    plan.norms(g, sums)
+    want = [float((g[o:o + k].double() ** 2).sum()) for o, k in zip(offs.tolist(), numels.tolist())]
+    got = sums.cpu().numpy()
+    assert np.allclose(got[:4], want, rtol=1e-12, atol=0) and np.isclose(got[4], sum(want), rtol=1e-12, atol=0)
+    kind = torch.uint8 if coded else torch.float32
+
+    def fresh(blocks):
+        st = [p.clone(), torch.zeros(n, dtype=kind, device="cuda"), torch.zeros(n, dtype=kind, device="cuda")]
+        return st + ([torch.zeros(2 * blocks, dtype=torch.uint8, device="cuda")] if coded else [])
+
+    whole, step = fresh(plan.blocks), torch.zeros(1, dtype=torch.int64, device="cuda")
+    f = plan.adamw_coded if coded else plan.adamw
+    for _ in range(2):
+        f(s, g, *whole, step, d_sumsq=sums)
+    assert int(step) == 2
+    first = 0
+    for l, (o, k) in enumerate(zip(offs.tolist(), numels.tolist())):
+        one = B.Optim(table(B, [o], [k]), [[1.0, 0.5, 2.0, 1.0][l]], [[1.0, 0.0, 1.0, 0.5][l]])
+        st, step = fresh(one.blocks), torch.zeros(1, dtype=torch.int64, device="cuda")
+        f = one.adamw_coded if coded else one.adamw
+        for _ in range(2):
+            f(s, g, *st, step, d_sumsq=torch.stack((sums[l], sums[4])))
+        for a, b in zip(whole[:3], st[:3]):
+            assert torch.equal(a[o:o + k], b[o:o + k]), l
+        if coded:
+            assert torch.equal(whole[3][first:first + 2 * one.blocks], st[3])
+            first += 2 * one.blocks
+        assert int(step) == 2
+    bad = g.clone()
+    bad[-3] = float("inf")                              # the last layer's only element
+    plan.norms(bad, sums)
+    old = [a.clone() for a in whole]
+    step = torch.tensor([5], device="cuda")
+    f = plan.adamw_coded if coded else plan.adamw
+    f(s, bad, *whole, step, d_sumsq=sums)
+    assert int(step) == 5 and all(torch.equal(a, b) for a, b in zip(old, whole))
+
+
+@pytest.mark.parametrize("layers", [64, 65, 4096, 4097, 20000])
+def test_many_layers(layers):
+    """Norms and a step of thousands of short layers, twice over one plan."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    rng = np.random.default_rng(layers)
+    numels = rng.integers(1, 40, layers)
+    numels[::997] = 20000
+    offs = np.cumsum(numels) - numels
+    n = int(numels.sum())
+    g, p, m, v = values(rng, n, offs, numels)
+    plan = B.Optim(table(B, offs, numels))
+    d = [torch.from_numpy(a).cuda() for a in (g, p, m, v)]
+    sums, step = torch.zeros(layers + 1, dtype=torch.float64, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    want = np.add.reduceat(g.astype(np.float64) ** 2, offs)
+    for k in range(2):
+        sums.fill_(-1.0)
+        plan.norms(d[0], sums)
+        got = sums.cpu().numpy()
+        assert np.allclose(got[:-1], want, rtol=1e-12, atol=0) and np.isclose(got[-1], want.sum(), rtol=1e-12, atol=0)
+        plan.adamw(B.adamw(lr=1e-3, weight_decay=0.0), *d, step, d_sumsq=sums)
+        new, tol = bounds(g, p, m, v, k + 1, 1e-3, 0.0, 1.0)
+        p, m, v = (a.cpu().numpy() for a in d[1:])
+        for a, w, e, what in zip((p, m, v), new, tol, "pmv"):
+            near(a, w, e, what)
+    assert int(step) == 2
+
+
 # ------------------------------------------------------------------------------ streams, graphs, far offsets, refusals
 def test_far_offsets():
     """Layers beyond 2^32 elements into the buffers."""
