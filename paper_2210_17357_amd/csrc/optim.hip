@@ -24,7 +24,12 @@ constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
 constexpr int kNormPart = 16384, kNormParts = 6000;
 constexpr int kStepPart = 4 * kThreads;        // elements of a workgroup of the step: one access a thread and buffer
 constexpr int kCodedPart = 8 * kThreads;       // the same with 8-bit moments
-constexpr int kShortParts = 16384;          // most workgroups of a step that works out its own factors
+constexpr int kShortParts = 65536;             // most workgroups of a step that works out its own factors
+// Longer steps ask for LDS that they do not use, so that 3 workgroups (5 with 8-bit moments) share a compute unit and not 8: the
+// chip's accesses then stay in a narrower window of memory.  355 M elements, us, with 8 / 6 / 5 / 4 / 3 / 2: fp32 moments
+// 1730 / 1685 / 1650 / 1640 / 1615 / 1675, 8-bit ones 990 / 978 / 933 / 928 / 980 / 1258; 150 M 741 / 721 / 700 / 697 / 682 /
+// 682 and 411 / 397 / 409 / 404 / 421 / 515.  Below 80 M elements it makes no difference.
+constexpr size_t kStepLds = 52 << 10, kCodedLds = 31 << 10;
 constexpr int64_t kMaxParts = ((int64_t)1 << 32) / kThreads - 1;   // (a launch takes fewer than 2^32 threads)
 constexpr int kLine = 32;            // elements of a 128-byte line of fp32
 
@@ -64,6 +69,7 @@ constexpr int kFactorWords = sizeof(StepFactors) / 4;
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
 struct BF16 { uint16_t bits; };
@@ -145,17 +151,17 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(NoCopy*, float) {}
 
 // ------------------------------------------------------------------ the last workgroup
-// Whether the caller is the last of n that ask, the i-th one: a ticket among 64 neighbours, then one of their groups, so that no
-// word of memory takes more than 64 of them (one word for 4000 workgroups: 30 us where these take 12).  The last ones clear the words for the next launch.  (Of more than 64 * 64,
-// groups are larger.)
+// Whether the caller is the last of n that ask, the i-th one: a ticket among 64 neighbours or more, then one of their at most 256
+// groups, so that no word of memory takes many at a time (one word for 4000 workgroups: 30 us where these take 12).  The
+// last ones clear the words for the next launch.
 // Tickets order nothing by themselves: an ordered one writes back and drops the L2 caches, which took the norms of 355 M
 // elements from 212 to 360 us.  What the last one reads is published by an exchange, which is performed where all caches
 // meet before it returns, and read by loads of the same scope.
-constexpr int kTicketGroup = 64;
+constexpr uint32_t kTicketGroup = 64, kTicketGroups = 256;
 constexpr int kTicketLine = 32;                                // words apart
-constexpr int kTicketWords = kTicketLine * (1 + kTicketGroup);
 __host__ __device__ inline uint32_t ticket_group(uint32_t n) {
-    return n > kTicketGroup * kTicketGroup ? (n + kTicketGroup - 1) / kTicketGroup : kTicketGroup;
+    const uint32_t even = (n + kTicketGroups - 1) / kTicketGroups;
+    return even > kTicketGroup ? even : kTicketGroup;
 }
 __host__ __device__ inline uint32_t ticket_lines(uint32_t n) { return n <= kTicketGroup ? 1 : 1 + (n + ticket_group(n) - 1) / ticket_group(n); }
 __device__ __forceinline__ bool last_drawn(uint32_t* word, uint32_t n) {
@@ -209,15 +215,27 @@ __global__ __launch_bounds__(kThreads) void norms_kernel(NormParams k) {
     const NormPart t = k.parts[blockIdx.x];
     const G* const g = static_cast<const G*>(k.grads) + t.start;
     const int tid = threadIdx.x;
-    constexpr int kWide = 16 / sizeof(G);
+    // four accesses of a thread in flight; past the end a thread reads the last whole access again and adds nothing
+    constexpr int kWide = 16 / sizeof(G), kAhead = 4, kRound = kWide * kThreads;
     double a[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 4
-    for (int i = kWide * tid; i + kWide <= t.count; i += kWide * kThreads) {
-        float x[kWide];
-        load16(g + i, x);
+    const int last = t.count - kWide;
+    const auto batch = [&](int first, bool whole) __attribute__((always_inline)) {
+        float x[kAhead][kWide];
 #pragma unroll
-        for (int j = 0; j < kWide; ++j) a[j & 3] = __builtin_fma((double)x[j], (double)x[j], a[j & 3]);
-    }
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = first + u * kRound + kWide * tid;
+            load16(g + (whole ? i : min(i, last)), x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (!whole && first + u * kRound + kWide * tid > last) continue;
+#pragma unroll
+            for (int j = 0; j < kWide; ++j) a[j & 3] = __builtin_fma((double)x[u][j], (double)x[u][j], a[j & 3]);
+        }
+    };
+    int first = 0;
+    for (; first + kAhead * kRound <= t.count; first += kAhead * kRound) batch(first, true);
+    if (first <= last) batch(first, false);
     if (tid < t.count % kWide) {
         const double x = (double)widen(g[t.count / kWide * kWide + tid]);
         a[0] = __builtin_fma(x, x, a[0]);
@@ -251,15 +269,14 @@ struct FactorParams {
 };
 
 __device__ __forceinline__ StepFactors factors_of(const FactorParams& p) {
+    // (all three on their way before one is used)
+    const double s = p.total ? *p.total : 0.0;
+    const float lr_factor = p.lr_factor ? *p.lr_factor : 1.0f;
+    const uint64_t t = (uint64_t)(*p.step + 1);
     StepFactors f{};
     double c = p.grad_scale;
-    f.go = 1;
-    if (p.total) {
-        const double s = *p.total;
-        if (!(s <= DBL_MAX)) f.go = 0;                           // NaN or infinite
-        if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * sqrt(s) + 1e-6));
-    }
-    const uint64_t t = (uint64_t)(*p.step + 1);
+    f.go = s <= DBL_MAX;                                         // neither NaN nor infinite
+    if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * sqrt(s) + 1e-6));
     // b^t by squaring: its relative error is some t 2^-53, and b^t is 0 long before that matters
     double power1 = 1.0, power2 = 1.0, b1 = p.beta1, b2 = p.beta2;
     for (uint64_t n = t; n; n >>= 1) {
@@ -270,7 +287,7 @@ __device__ __forceinline__ StepFactors factors_of(const FactorParams& p) {
         b1 *= b1;
         b2 *= b2;
     }
-    f.lr = p.lr_factor ? p.lr * (double)*p.lr_factor : p.lr;
+    f.lr = p.lr * (double)lr_factor;
     f.lr_m = f.lr / (1.0 - power1);
     f.root_v = (float)(1.0 / sqrt(1.0 - power2));
     f.grad = (float)c;
@@ -463,18 +480,15 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     uint8_t* const exps = k.exps + 2 * (t.block + i / kOptimBlock);
 
     float gi[8], pi[8], mi[8], vi[8];
-    uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
-    int xm = 0, xv = 0;
-    if (left > 0) {
-        xm = exps[0];
-        xv = exps[1];
-    }
+    uint32_t cm[2] = {0, 0}, cv[2] = {0, 0}, x = 0;          // (x: both exponents, taken apart when everything is on its way)
     if (whole) {
+        x = *reinterpret_cast<const u16_any*>(exps);
         load8(g, gi);
         load8(p, pi);
         load8(m, cm);
         load8(v, cv);
     } else {
+        if (left > 0) x = *reinterpret_cast<const u16_any*>(exps);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool in = place(j) < left;
@@ -488,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     if (!f.go) return;
     const Rates r = rates_of(f, k, t);
     // (elements past the layer's end: gradient 0 and codes 0, so their moments are 0)
-    decode8(cm, cv, xm, xv, mi, vi);
+    decode8(cm, cv, (int)(x & 255u), (int)(x >> 8), mi, vi);
     float top_m = 0.0f, top_v = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) step_one(k, r, gi[j], pi[j], mi[j], vi[j]);
@@ -497,8 +511,8 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
         top_m = max3_abs(mi[j], mi[j + 1], top_m);
         top_v = max3f(vi[j], vi[j + 1], top_v);
     }
-    xm = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_m)));
-    xv = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_v)));
+    const int xm = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_m)));
+    const int xv = block_exponent(__builtin_bit_cast(uint32_t, row16_max(top_v)));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         Philox4 words{};
@@ -518,8 +532,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     }
     if (left <= 0) return;
     if (lane == 0) {
-        exps[0] = (uint8_t)xm;
-        exps[1] = (uint8_t)xv;
+        *reinterpret_cast<u16_any*>(exps) = (uint16_t)(xm | xv << 8);
     }
     if (whole) {
         store8(m, cm);
@@ -556,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restric
     const uint8_t* const x = exps + 2 * (t.block + first / kOptimBlock);
     O* const mo = m_out + t.start + i;
     O* const vo = v_out + t.start + i;
-    const int xm = x[0], xv = x[1];
+    const uint32_t both = *reinterpret_cast<const u16_any*>(x);
     if (first + kOptimBlock <= t.count) {
         uint32_t cm[2], cv[2];
         float fm[8], fv[8];
@@ -567,7 +580,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restric
             load8(m, cm);
             load8(v, cv);
         }
-        decode8(cm, cv, xm, xv, fm, fv);
+        decode8(cm, cv, (int)(both & 255u), (int)(both >> 8), fm, fv);
         if constexpr (kRun) {
             store16(mo, fm);
             store16(vo, fv);
@@ -579,17 +592,17 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restric
         for (int j = 0; j < 8; ++j) {
             const int at = kRun ? j : place(j);
             if (at >= left) break;
-            store1(mo + at, decoded_m(m[at], xm));
-            store1(vo + at, decoded_v(v[at], xv));
+            store1(mo + at, decoded_m(m[at], (int)(both & 255u)));
+            store1(vo + at, decoded_v(v[at], (int)(both >> 8)));
         }
     }
 }
 
 // A launch's own error, whatever another call on this thread left behind.
 template <typename... A>
-hipError_t launch(void (*kernel)(A...), int64_t grid, int threads, hipStream_t s, A... args) {
+hipError_t launch(void (*kernel)(A...), int64_t grid, int threads, size_t lds, hipStream_t s, A... args) {
     void* list[] = {&args...};
-    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), list, 0, s);
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3(threads), list, lds, s);
 }
 
 size_t element_size(int32_t type) { return type == LGRECO_F32 ? 4 : 2; }
@@ -684,7 +697,7 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
     HIPCHK(to_device(&o->d_coded, coded));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_partials), sizeof(double) * norm.size()));
     HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_factors), sizeof(StepFactors)));
-    HIPCHK(to_device(&o->d_tickets, std::vector<uint32_t>(kTicketWords, 0u)));
+    HIPCHK(to_device(&o->d_tickets, std::vector<uint32_t>((size_t)kTicketLine * (1 + kTicketGroups), 0u)));
     HIPCHK(to_device(&o->d_norm_tickets, std::vector<uint32_t>(norm_tickets, 0u)));
     return LGRECO_OK;
 }
@@ -720,7 +733,7 @@ int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int3
     *k = StepParams{parts, short_table ? nullptr : o->d_factors, raw, o->d_tickets, grads, params, const_cast<void*>(m),
                     const_cast<void*>(v), nullptr, const_cast<void*>(copy), c->weight_decay, (float)c->beta1, (float)(1.0 - c->beta1),
                     (float)c->beta2, (float)(1.0 - c->beta2), (float)c->eps, c->stochastic, (uint32_t)c->seed, (uint32_t)(c->seed >> 32)};
-    if (!short_table) HIPCHK(launch(factors_kernel, 1, 64, s, raw, o->d_factors));
+    if (!short_table) HIPCHK(launch(factors_kernel, 1, 64, 0, s, raw, o->d_factors));
     return LGRECO_OK;
 }
 
@@ -781,7 +794,7 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
     if (st != LGRECO_OK) return st;
     hipStream_t s = (hipStream_t)stream;
     const NormParams k{o->d_norm, d_grads, o->d_partials, d_sumsq, o->L, o->d_norm_tickets};
-    HIPCHK(launch(grad_type == LGRECO_F32 ? norms_kernel<float> : norms_kernel<BF16>, o->n_norm, kThreads, s, k));
+    HIPCHK(launch(grad_type == LGRECO_F32 ? norms_kernel<float> : norms_kernel<BF16>, o->n_norm, kThreads, 0, s, k));
     return LGRECO_OK;
 }
 
@@ -794,7 +807,7 @@ int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void*
     const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 4, d_copy, copy_type, d_sumsq, d_lr, d_step, s, o->d_step, o->n_step, &k);
     if (st != LGRECO_OK) return st;
     const StepKernel f = grad_type == LGRECO_F32 ? adamw_kernel_of<float>(d_copy, copy_type) : adamw_kernel_of<BF16>(d_copy, copy_type);
-    HIPCHK(launch(f, o->n_step, kThreads, s, k));
+    HIPCHK(launch(f, o->n_step, kThreads, k.factors ? kStepLds : 0, s, k));
     return LGRECO_OK;
 }
 
@@ -813,7 +826,7 @@ int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const
         f = grad_type == LGRECO_F32 ? coded_kernel_of<float, true>(d_copy, copy_type) : coded_kernel_of<BF16, true>(d_copy, copy_type);
     else
         f = grad_type == LGRECO_F32 ? coded_kernel_of<float, false>(d_copy, copy_type) : coded_kernel_of<BF16, false>(d_copy, copy_type);
-    HIPCHK(launch(f, o->n_coded, kThreads, s, k));
+    HIPCHK(launch(f, o->n_coded, kThreads, k.factors ? kCodedLds : 0, s, k));
     return LGRECO_OK;
 }
 
@@ -826,10 +839,10 @@ int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_
     hipStream_t s = (hipStream_t)stream;
     const Part* const parts = o->d_coded;
     if (type == LGRECO_F32)
-        HIPCHK(launch(moments_kernel<float>, o->n_coded, kThreads, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
+        HIPCHK(launch(moments_kernel<float>, o->n_coded, kThreads, 0, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
                       static_cast<float*>(d_v_out)));
     else
-        HIPCHK(launch(moments_kernel<BF16>, o->n_coded, kThreads, s, parts, d_m, d_v, d_exps, static_cast<BF16*>(d_m_out),
+        HIPCHK(launch(moments_kernel<BF16>, o->n_coded, kThreads, 0, s, parts, d_m, d_v, d_exps, static_cast<BF16*>(d_m_out),
                       static_cast<BF16*>(d_v_out)));
     return LGRECO_OK;
 }
