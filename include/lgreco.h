@@ -399,7 +399,8 @@ int lgreco_last_solve_groups(const lgreco_handle_t* h);
  * buffers it was captured with; the step count and the learning rate's factor are read from the
  * device.  Calls on one plan share its scratch: they, and replays of graphs that hold them, must not
  * overlap in time.  A plan is used with the device current that was current at its creation (another
- * one: LGRECO_EINVAL), and destroyed when none of its calls or graphs is in use any more.
+ * one: LGRECO_EINVAL), on streams of that device, and destroyed when none of its calls or graphs is in use any
+ * more.  Creating or destroying one allocates or frees device memory: not while a stream is being captured.
  *
  * The buffers d_grads, d_params, d_m, d_v and d_copy have the layout of the table: layer l is
  * the elements [offset, offset + numel) of each.  They must not overlap.  Elements outside the
@@ -457,7 +458,7 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
  *              NaN or infinite, the step is left out: no buffer and no step count changes.
  *              Required with max_norm > 0.
  *   d_lr       fp32 on the device, multiplies lr (a schedule that replays follow), or NULL (= 1)
- *   d_step     int64 on the device: steps taken so far, in/out */
+ *   d_step     int64 on the device: steps taken so far (>= 0), in/out */
 int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
                        float* d_params, float* d_m, float* d_v, void* d_copy, int32_t copy_type,
                        const double* d_sumsq, const float* d_lr, int64_t* d_step, void* stream);

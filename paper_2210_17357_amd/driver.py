@@ -63,7 +63,8 @@ class AdamW:
     """Parameters' update behind the exchange: moments (fp32, or 8 bits with `coded`), step count and norms of the
     layers of one flat parameter buffer.  `layers` are all the tensors to be stepped, also those that travel
     uncompressed.  With `guard` (always with clipping) a step whose gradients are not finite is left out.
-    Nothing waits for the GPU in `step`; it may be captured into a HIP graph."""
+    Nothing waits for the GPU in `step`; it may be captured into a HIP graph.  The state is made and read out on torch's
+    current stream: a caller whose steps run on another one orders the two."""
 
     def __init__(self, layers, d_params, settings: "B.AdamW", lr_scale=None, decay_scale=None, coded: bool = False,
                  d_copy=None, guard: bool = False):
@@ -96,11 +97,11 @@ class AdamW:
             handle.decompress(payload, offsets, layers, cands, choice, d_grads, accumulate=w > 0, stream=stream)
         self.step(d_grads, d_lr=d_lr, stream=stream)
 
-    def moments(self, stream=None):
-        """The moments as fp32 tensors (elements outside the layers: zero)."""
+    def moments(self):
+        """The moments as new fp32 tensors (elements outside the layers: zero)."""
         if not self.coded:
             return self.d_m.clone(), self.d_v.clone()
         import torch
         out = [torch.zeros(self.d_m.numel(), dtype=torch.float32, device=self.d_m.device) for _ in range(2)]
-        self.plan.decode(self.d_m, self.d_v, self.d_exps, *out, stream=stream)
+        self.plan.decode(self.d_m, self.d_v, self.d_exps, *out)
         return tuple(out)

@@ -493,12 +493,13 @@ def test_decode(name, kind):
 
 # ------------------------------------------------------------------------------ long tables
 @pytest.mark.parametrize("coded", [False, True])
-def test_a_long_table_is_its_layers_one_by_one(coded):
-    """More workgroups than work out their own factors, layers of more than 64 parts: bit for bit what plans of one layer
-    each give."""
+@pytest.mark.parametrize("largest", [40_000_003, 140_000_003])
+def test_a_long_table_is_its_layers_one_by_one(coded, largest):
+    """Tables whose workgroups work out their own factors and tables beyond 65536 workgroups, which leave that to a kernel in
+    front; layers of more than 64 parts: bit for bit what plans of one layer each give."""
     from paper_2210_17357_amd import binding as B
     torch = torch_cuda()
-    numels = np.array([40_000_003, 77, 2_500_001, 1])
+    numels = np.array([largest, 77, 2_500_001, 1])
     offs = np.cumsum(numels + 1) - numels
     n = int(offs[-1] + numels[-1]) + 2
     gen = torch.Generator(device="cuda").manual_seed(16)
@@ -728,6 +729,45 @@ def test_receive_is_the_sum_of_the_workers_and_a_step(coded, max_norm):
                 near(run.d_m.cpu().numpy()[cut], new[1], tol[1], ("m", t, l))
                 near(run.d_v.cpu().numpy()[cut], new[2], tol[2], ("v", t, l))
         assert torch.equal(run.d_copy, run.d_params.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_captured_steps_of_a_long_table(coded):
+    """The same for a table beyond 65536 workgroups, against eager steps of another plan."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    n = 140_000_001 if coded else 70_000_001
+    layers = table(B, [0], [n])
+    plans = [B.Optim(layers), B.Optim(layers)]
+    s = B.adamw(lr=1e-2, max_norm=0.5, stochastic=True, seed=1)
+    kind = torch.uint8 if coded else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    g = torch.zeros(n, device="cuda")
+    state = [{"p": torch.ones(n, device="cuda"), "m": torch.zeros(n, dtype=kind, device="cuda"), "v": torch.zeros(n, dtype=kind, device="cuda"),
+              "x": torch.zeros(2 * plans[0].blocks, dtype=torch.uint8, device="cuda"), "step": torch.zeros(1, dtype=torch.int64, device="cuda"),
+              "sums": torch.zeros(2, dtype=torch.float64, device="cuda")} for _ in plans]
+
+    def once(plan, d):
+        plan.norms(g, d["sums"])
+        if coded:
+            plan.adamw_coded(s, g, d["p"], d["m"], d["v"], d["x"], d["step"], d_sumsq=d["sums"])
+        else:
+            plan.adamw(s, g, d["p"], d["m"], d["v"], d["step"], d_sumsq=d["sums"])
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once(plans[0], state[0])
+    for k in range(4):
+        g.normal_(generator=gen)
+        if k == 2:
+            g[n - 1] = float("inf")
+        graph.replay()
+        once(plans[1], state[1])
+        torch.cuda.synchronize()
+        for key in ("p", "m", "v", "x", "step", "sums"):
+            assert torch.equal(state[0][key], state[1][key]), (k, key)
+    assert int(state[0]["step"]) == 3
 
 
 def test_on_another_stream():
