@@ -426,7 +426,7 @@ typedef struct {
     int32_t  reserved;      /* must be 0 */
 } lgreco_adamw_t;
 
-/* Creates a plan for these layers on the current device.  It takes about 64 bytes of device memory for every 1024 elements
+/* Creates a plan for these layers on the current device.  It takes about 45 bytes of device memory for every 1024 elements
  * and 130 for every layer; tables of more than 2^24 - 1 pieces of 1024 elements (17 G elements): LGRECO_ENOSPACE.
  *   lr_scale     host [L] factors of lr per layer, or NULL (= 1): finite, >= 0
  *   decay_scale  host [L] factors of weight_decay per layer, or NULL (= 1): finite, >= 0 */

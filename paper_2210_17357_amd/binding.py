@@ -408,7 +408,8 @@ class Optim:
         if st != OK:
             raise LgrecoError(st, strerror(st))
         self.L = len(layers)
-        self.extent = max(a.offset + a.numel for a in layers)
+        at = np.frombuffer(layers, np.dtype([("offset", "i8"), ("numel", "i8"), ("shape", "i4", 2)]))
+        self.extent = int((at["offset"] + at["numel"]).max())
         self.blocks = int(lib().lgreco_optim_blocks(self._o))
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         self._f32, self._f64, self._u8, self._i64 = torch.float32, torch.float64, torch.uint8, torch.int64

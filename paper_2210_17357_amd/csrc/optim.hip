@@ -8,8 +8,9 @@
 #include <cfloat>
 #include <cmath>
 #include <cstdio>
+#include <cstring>
+#include <memory>
 #include <new>
-#include <vector>
 
 #include "internal.h"
 
@@ -42,14 +43,18 @@ struct NormPart {
 };
 
 // What one workgroup of the step works on: consecutive elements of one layer.
-struct Part {
+struct StepPart {
     int64_t start;       // first element, into the flat buffers
-    int64_t block;       // 8-bit moments: its first block
     int32_t count;       // elements
-    int32_t pos;         // first element, relative to the layer start
-    int32_t layer;
     float lr_scale, decay_scale;
     int32_t pad;
+};
+struct CodedPart {       // the same with 8-bit moments
+    int64_t start;
+    int32_t count;
+    float lr_scale, decay_scale;
+    int32_t layer, pos;  // pos: first element, relative to the layer start
+    int32_t block;       // its first block
 };
 
 // The step's factors that are the same for all elements, worked out on the device (the step count, the norm and the
@@ -304,7 +309,7 @@ __global__ __launch_bounds__(64) void factors_kernel(FactorParams p, StepFactors
 
 // ------------------------------------------------------------------ AdamW
 struct StepParams {
-    const Part* parts;
+    const void* parts;             // StepPart or CodedPart
     const StepFactors* factors;    // null: the workgroups work them out themselves
     FactorParams raw;
     uint32_t* tickets;
@@ -353,7 +358,8 @@ struct Rates {
     float rate;          // lr / (1 - b1^t)
     float grad, root_v;
 };
-__device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams& p, const Part& t) {
+template <typename P>
+__device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams& p, const P& t) {
     const double s = (double)t.lr_scale;
     return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v};
 }
@@ -375,7 +381,7 @@ __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, fl
 // both rounds' loads ahead, 1955 without the streaming hints.
 template <typename G, typename C>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
-    const Part t = k.parts[blockIdx.x];
+    const StepPart t = static_cast<const StepPart*>(k.parts)[blockIdx.x];
     const int i = 4 * threadIdx.x, left = t.count - i;
     const G* const g = static_cast<const G*>(k.grads) + t.start + i;
     float* const p = k.p + t.start + i;
@@ -471,7 +477,7 @@ __device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t 
 // consecutive elements, whose fp32 accesses are half lines: 1100; the codes' accesses with streaming hints: 1 to 3 % more.)
 template <typename G, typename C, bool STOCHASTIC>
 __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
-    const Part t = k.parts[blockIdx.x];
+    const CodedPart t = static_cast<const CodedPart*>(k.parts)[blockIdx.x];
     const int lane = threadIdx.x & 15, i = threadIdx.x / 16 * kOptimBlock + 4 * lane, left = t.count - i;
     const bool whole = i - 4 * lane + kOptimBlock <= t.count;
     const G* const g = static_cast<const G*>(k.grads) + t.start + i;
@@ -479,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     uint8_t* const m = static_cast<uint8_t*>(k.m) + t.start + i;
     uint8_t* const v = static_cast<uint8_t*>(k.v) + t.start + i;
     C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
-    uint8_t* const exps = k.exps + 2 * (t.block + i / kOptimBlock);
+    uint8_t* const exps = k.exps + 2 * (int64_t)(t.block + i / kOptimBlock);
 
     float gi[8], pi[8], mi[8], vi[8];
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0}, x = 0;          // (x: both exponents, taken apart when everything is on its way)
@@ -558,17 +564,17 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
 // Bound by HBM.  A row of 16 lanes takes a block; for 16-bit values a lane takes 8 consecutive elements, one access of each
 // buffer (355 M elements: 365 us, 5.8 TB/s, 390 as for fp32).
 template <typename O>
-__global__ __launch_bounds__(kThreads) void moments_kernel(const Part* __restrict__ parts, const uint8_t* __restrict__ codes_m,
+__global__ __launch_bounds__(kThreads) void moments_kernel(const CodedPart* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
                                                            O* __restrict__ m_out, O* __restrict__ v_out) {
     constexpr bool kRun = sizeof(O) == 2;
-    const Part t = parts[blockIdx.x];
+    const CodedPart t = parts[blockIdx.x];
     const int lane = threadIdx.x & 15, first = threadIdx.x / 16 * kOptimBlock;
     const int i = first + (kRun ? 8 : 4) * lane, left = t.count - i;
     if (left <= 0) return;
     const uint8_t* const m = codes_m + t.start + i;
     const uint8_t* const v = codes_v + t.start + i;
-    const uint8_t* const x = exps + 2 * (t.block + first / kOptimBlock);
+    const uint8_t* const x = exps + 2 * (int64_t)(t.block + first / kOptimBlock);
     O* const mo = m_out + t.start + i;
     O* const vo = v_out + t.start + i;
     const uint32_t both = *reinterpret_cast<const u16_any*>(x);
@@ -620,9 +626,10 @@ struct lgreco_optim {
     int32_t L = 0;
     int64_t blocks = 0;
     int64_t n_norm = 0, n_step = 0, n_coded = 0;   // parts of the three cuts of the table
+    uint8_t* d_all = nullptr;                      // one allocation, of
     NormPart* d_norm = nullptr;
-    Part* d_step = nullptr;                        // cut on whole lines of the flat buffers
-    Part* d_coded = nullptr;                       // cut on the layers' blocks
+    StepPart* d_step = nullptr;                    // cut on whole lines of the flat buffers
+    CodedPart* d_coded = nullptr;                  // cut on the layers' blocks
     double* d_partials = nullptr;                  // [n_norm]
     StepFactors* d_factors = nullptr;
     uint32_t* d_tickets = nullptr;                 // of the step; zero between launches, like
@@ -653,54 +660,74 @@ void for_parts(const lgreco_layer_t& a, int64_t part, int64_t line, F f) {
     }
 }
 
-template <typename T>
-hipError_t to_device(T** d, const std::vector<T>& h) {
-    hipError_t e = hipMalloc(reinterpret_cast<void**>(d), sizeof(T) * h.size());
-    return e != hipSuccess ? e : hipMemcpy(*d, h.data(), sizeof(T) * h.size(), hipMemcpyHostToDevice);
+int64_t count_parts(const lgreco_layer_t& a, int64_t part, int64_t line) {
+    const int64_t head = part - a.offset % line;
+    return a.numel <= head ? 1 : 1 + (a.numel - head + part - 1) / part;
 }
 
 int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float* lr_scale, const float* decay_scale) {
     const int st = check_layers(layers, L);
     if (st != LGRECO_OK) return st;
-    std::vector<NormPart> norm;
-    std::vector<Part> step, coded;
-    size_t norm_tickets = (size_t)kTicketLine * ticket_lines((uint32_t)L);
     int64_t total = 0;
     for (int32_t l = 0; l < L; ++l) total += layers[l].numel;
     int64_t norm_part = kNormPart;
     while (total / norm_part > kNormParts) norm_part *= 2;
+    size_t norm_words = (size_t)kTicketLine * ticket_lines((uint32_t)L);
+    for (int32_t l = 0; l < L; ++l) {
+        const lgreco_layer_t& a = layers[l];
+        if (a.offset > ((int64_t)1 << 58)) return LGRECO_EINVAL;            // (in bytes, beyond any address)
+        for (const float* f : {lr_scale, decay_scale})
+            if (f && !(f[l] >= 0.0f && f[l] <= FLT_MAX)) return LGRECO_EINVAL;
+        const int64_t parts = count_parts(a, norm_part, kLine);
+        if (parts > 1) norm_words += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
+        o->n_norm += parts;
+        o->n_step += count_parts(a, kStepPart, kLine);
+        o->n_coded += count_parts(a, kCodedPart, 1);
+    }
+    if (o->n_step > kMaxParts) return LGRECO_ENOSPACE;                      // (the finest of the cuts)
+    o->L = L;
+    HIPCHK(hipGetDevice(&o->device));
+
+    // one allocation: first what the host writes (the tickets as zeros), then the scratch
+    size_t bytes = 0;
+    const auto room = [&](size_t n) {
+        const size_t at = bytes;
+        bytes += (n + 127) / 128 * 128;
+        return at;
+    };
+    const size_t norm_at = room(sizeof(NormPart) * o->n_norm), step_at = room(sizeof(StepPart) * o->n_step),
+                 coded_at = room(sizeof(CodedPart) * o->n_coded), tickets_at = room(4 * (size_t)kTicketLine * (1 + kTicketGroups)),
+                 norm_tickets_at = room(4 * norm_words), written = bytes;
+    const size_t partials_at = room(sizeof(double) * o->n_norm), factors_at = room(sizeof(StepFactors));
+    const std::unique_ptr<uint8_t[]> host(new uint8_t[written]);
+    std::memset(&host[tickets_at], 0, written - tickets_at);
+    NormPart* norm = reinterpret_cast<NormPart*>(&host[norm_at]);
+    StepPart* step = reinterpret_cast<StepPart*>(&host[step_at]);
+    CodedPart* coded = reinterpret_cast<CodedPart*>(&host[coded_at]);
+    size_t word = (size_t)kTicketLine * ticket_lines((uint32_t)L);
     for (int32_t l = 0; l < L; ++l) {
         const float ls = lr_scale ? lr_scale[l] : 1.0f, ds = decay_scale ? decay_scale[l] : 1.0f;
-        if (!(ls >= 0.0f && ls <= FLT_MAX) || !(ds >= 0.0f && ds <= FLT_MAX)) return LGRECO_EINVAL;
-        if (layers[l].offset > ((int64_t)1 << 58)) return LGRECO_EINVAL;     // (in bytes, beyond any address)
-        const size_t first = norm.size();
+        const int32_t parts = (int32_t)count_parts(layers[l], norm_part, kLine);
+        int32_t index = 0;
         for_parts(layers[l], norm_part, kLine, [&](int64_t start, int64_t, int64_t n) {
-            norm.push_back(NormPart{start, (int32_t)n, l, (int32_t)(norm.size() - first), 0, (int32_t)norm_tickets, 0});
+            *norm++ = NormPart{start, (int32_t)n, l, index++, parts, (int32_t)word, 0};
         });
-        const size_t parts = norm.size() - first;
-        for (size_t i = first; i < norm.size(); ++i) norm[i].parts = (int32_t)parts;
-        if (parts > 1) norm_tickets += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
-        for_parts(layers[l], kStepPart, kLine, [&](int64_t start, int64_t pos, int64_t n) {
-            step.push_back(Part{start, 0, (int32_t)n, (int32_t)pos, l, ls, ds, 0});
-        });
+        if (parts > 1) word += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
+        for_parts(layers[l], kStepPart, kLine, [&](int64_t start, int64_t, int64_t n) { *step++ = StepPart{start, (int32_t)n, ls, ds, 0}; });
         for_parts(layers[l], kCodedPart, 1, [&](int64_t start, int64_t pos, int64_t n) {
-            coded.push_back(Part{start, o->blocks + pos / kOptimBlock, (int32_t)n, (int32_t)pos, l, ls, ds, 0});
+            *coded++ = CodedPart{start, (int32_t)n, ls, ds, l, (int32_t)pos, (int32_t)(o->blocks + pos / kOptimBlock)};
         });
         o->blocks += (layers[l].numel + kOptimBlock - 1) / kOptimBlock;
-        if ((int64_t)step.size() > kMaxParts) return LGRECO_ENOSPACE;       // (the finest of the cuts)
     }
-    o->L = L;
-    o->n_norm = (int64_t)norm.size();
-    o->n_step = (int64_t)step.size();
-    o->n_coded = (int64_t)coded.size();
-    HIPCHK(hipGetDevice(&o->device));
-    HIPCHK(to_device(&o->d_norm, norm));
-    HIPCHK(to_device(&o->d_step, step));
-    HIPCHK(to_device(&o->d_coded, coded));
-    HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_partials), sizeof(double) * norm.size()));
-    HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_factors), sizeof(StepFactors)));
-    HIPCHK(to_device(&o->d_tickets, std::vector<uint32_t>((size_t)kTicketLine * (1 + kTicketGroups), 0u)));
-    HIPCHK(to_device(&o->d_norm_tickets, std::vector<uint32_t>(norm_tickets, 0u)));
+    HIPCHK(hipMalloc(reinterpret_cast<void**>(&o->d_all), bytes));
+    HIPCHK(hipMemcpy(o->d_all, host.get(), written, hipMemcpyHostToDevice));
+    o->d_norm = reinterpret_cast<NormPart*>(o->d_all + norm_at);
+    o->d_step = reinterpret_cast<StepPart*>(o->d_all + step_at);
+    o->d_coded = reinterpret_cast<CodedPart*>(o->d_all + coded_at);
+    o->d_tickets = reinterpret_cast<uint32_t*>(o->d_all + tickets_at);
+    o->d_norm_tickets = reinterpret_cast<uint32_t*>(o->d_all + norm_tickets_at);
+    o->d_partials = reinterpret_cast<double*>(o->d_all + partials_at);
+    o->d_factors = reinterpret_cast<StepFactors*>(o->d_all + factors_at);
     return LGRECO_OK;
 }
 
@@ -720,7 +747,7 @@ bool valid(const lgreco_adamw_t* c) {
 // What both forms of the step check and queue in front of their kernel.
 int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int32_t grad_type, float* params, const void* m,
                const void* v, size_t moment_size, const void* copy, int32_t copy_type, const double* sumsq, const float* lr,
-               int64_t* step, hipStream_t s, const Part* parts, int64_t n_parts, StepParams* k) {
+               int64_t* step, hipStream_t s, const void* parts, int64_t n_parts, StepParams* k) {
     if (!c || !grads || !params || !m || !v || !step || !valid(c)) return LGRECO_EINVAL;
     if (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16) return LGRECO_EINVAL;
     if (copy && copy_type != LGRECO_BF16 && copy_type != LGRECO_F16) return LGRECO_EINVAL;
@@ -774,13 +801,7 @@ int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int3
 
 int lgreco_optim_destroy(lgreco_optim_t* o) {
     if (!o) return LGRECO_EINVAL;
-    (void)hipFree(o->d_norm);
-    (void)hipFree(o->d_step);
-    (void)hipFree(o->d_coded);
-    (void)hipFree(o->d_partials);
-    (void)hipFree(o->d_factors);
-    (void)hipFree(o->d_tickets);
-    (void)hipFree(o->d_norm_tickets);
+    (void)hipFree(o->d_all);
     delete o;
     return LGRECO_OK;
 }
@@ -839,7 +860,7 @@ int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_
     const int st = on_device(o);
     if (st != LGRECO_OK) return st;
     hipStream_t s = (hipStream_t)stream;
-    const Part* const parts = o->d_coded;
+    const CodedPart* const parts = o->d_coded;
     if (type == LGRECO_F32)
         HIPCHK(launch(moments_kernel<float>, o->n_coded, kThreads, 0, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
                       static_cast<float*>(d_v_out)));
