@@ -85,16 +85,17 @@ __device__ __forceinline__ float widen(BF16 x) { return __builtin_bit_cast(float
 __device__ __forceinline__ uint16_t narrow_bits(float x, BF16) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t narrow_bits(float x, F16) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 
-__device__ __forceinline__ float4 load4(const float* p) { return load_stream(p); }
-__device__ __forceinline__ float4 load4(const BF16* p) {
-    const u16x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
-    return make_float4(widen(BF16{v.x}), widen(BF16{v.y}), widen(BF16{v.z}), widen(BF16{v.w}));
-}
-// one 16-byte access
-__device__ __forceinline__ void load16(const float* p, float (&x)[4]) {
+__device__ __forceinline__ void load4(const float* p, float* x) {
     const float4 v = load_stream(p);
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
+__device__ __forceinline__ void load4(const BF16* p, float* x) {
+    const u16x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = widen(BF16{v[j]});
+}
+// one 16-byte access
+__device__ __forceinline__ void load16(const float* p, float (&x)[4]) { load4(p, x); }
 __device__ __forceinline__ void load16(const BF16* p, float (&x)[8]) {
     const u32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
 #pragma unroll
@@ -116,13 +117,14 @@ __device__ __forceinline__ void load_run(const uint8_t* p, uint32_t (&c)[2]) {
     c[1] = v.y;
 }
 template <typename C>
-__device__ __forceinline__ void store4(C* p, const float4 v) {
+__device__ __forceinline__ void store4(C* p, const float* x) {
     u16x4_any n;
-    n.x = narrow_bits(v.x, C{}); n.y = narrow_bits(v.y, C{}); n.z = narrow_bits(v.z, C{}); n.w = narrow_bits(v.w, C{});
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n[j] = narrow_bits(x[j], C{});
     __builtin_nontemporal_store(n, reinterpret_cast<u16x4_any*>(p));
 }
-__device__ __forceinline__ void store4(float* p, const float4 v) { store_stream(p, v); }
-__device__ __forceinline__ void store4(NoCopy*, const float4) {}
+__device__ __forceinline__ void store4(float* p, const float* x) { store_stream(p, make_float4(x[0], x[1], x[2], x[3])); }
+__device__ __forceinline__ void store4(NoCopy*, const float*) {}
 template <typename C>
 __device__ __forceinline__ C* shifted(C* p, int64_t n) { return p + n; }
 __device__ __forceinline__ NoCopy* shifted(NoCopy* p, int64_t) { return p; }
@@ -133,8 +135,8 @@ constexpr int kHalf = kOptimBlock / 2;
 __device__ __forceinline__ int place(int j) { return j < 4 ? j : kHalf - 4 + j; }
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-    const float4 a = load4(p), b = load4(p + kHalf);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    load4(p, x);
+    load4(p + kHalf, x + 4);
 }
 __device__ __forceinline__ void load8(const uint8_t* p, uint32_t (&c)[2]) {
     c[0] = *reinterpret_cast<const u32_any*>(p);
@@ -142,8 +144,8 @@ __device__ __forceinline__ void load8(const uint8_t* p, uint32_t (&c)[2]) {
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-    store4(p, make_float4(x[0], x[1], x[2], x[3]));
-    store4(shifted(p, kHalf), make_float4(x[4], x[5], x[6], x[7]));
+    store4(p, x);
+    store4(shifted(p, kHalf), x + 4);
 }
 __device__ __forceinline__ void store8(uint8_t* p, const uint32_t (&c)[2]) {
     *reinterpret_cast<u32_any*>(p) = c[0];
@@ -388,33 +390,41 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
     float* const m = static_cast<float*>(k.m) + t.start + i;
     float* const v = static_cast<float*>(k.v) + t.start + i;
     C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
-    float4 gi{}, pi{}, mi{}, vi{};
+    float gi[4]{}, pi[4]{}, mi[4]{}, vi[4]{};
     if (left >= 4) {
-        gi = load4(g);
-        pi = load4(p);
-        mi = load4(m);
-        vi = load4(v);
+        load4(g, gi);
+        load4(p, pi);
+        load4(m, mi);
+        load4(v, vi);
+    } else if (left > 0) {                                   // (the layer's last elements; what is read twice is stored once)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const int at = min(j, left - 1);
+            gi[j] = widen(g[at]);
+            pi[j] = p[at];
+            mi[j] = m[at];
+            vi[j] = v[at];
+        }
     }
     const StepFactors f = step_factors(k);
     if (!f.go) return;
     const Rates r = rates_of(f, k, t);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) step_one(k, r, gi[j], pi[j], mi[j], vi[j]);
     if (left >= 4) {
-        step_one(k, r, gi.x, pi.x, mi.x, vi.x);
-        step_one(k, r, gi.y, pi.y, mi.y, vi.y);
-        step_one(k, r, gi.z, pi.z, mi.z, vi.z);
-        step_one(k, r, gi.w, pi.w, mi.w, vi.w);
         store4(p, pi);
         store4(m, mi);
         store4(v, vi);
         store4(copy, pi);
     } else {
-        for (int j = 0; j < left; ++j) {
-            float pj = p[j], mj = m[j], vj = v[j];
-            step_one(k, r, widen(g[j]), pj, mj, vj);
-            p[j] = pj;
-            m[j] = mj;
-            v[j] = vj;
-            store1(shifted(copy, j), pj);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            if (j < left) {
+                p[j] = pi[j];
+                m[j] = mi[j];
+                v[j] = vi[j];
+                store1(shifted(copy, j), pi[j]);
+            }
         }
     }
     count_step(k, f);
@@ -487,27 +497,39 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
     C* const copy = shifted(static_cast<C*>(k.copy), t.start + i);
     uint8_t* const exps = k.exps + 2 * (int64_t)(t.block + i / kOptimBlock);
 
-    float gi[8], pi[8], mi[8], vi[8];
+    float gi[8]{}, pi[8]{}, mi[8], vi[8];
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0}, x = 0;          // (x: both exponents, taken apart when everything is on its way)
+    const bool some = (int)(threadIdx.x & ~63u) * 8 < t.count;     // whether the wavefront has elements
     if (whole) {
         x = *reinterpret_cast<const u16_any*>(exps);
         load8(g, gi);
         load8(p, pi);
         load8(m, cm);
         load8(v, cv);
-    } else {
-        if (left > 0) x = *reinterpret_cast<const u16_any*>(exps);
+    } else if (some) {
+        // a short block, and lanes behind the last one: everything is asked for at once, the part's last element in place of what is
+        // not there
+        const int last = left - 1;
+        uint32_t em[8], ev[8];
+        x = *reinterpret_cast<const u16_any*>(k.exps + 2 * (int64_t)(t.block + min(i, t.count - 1) / kOptimBlock));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool in = place(j) < left;
-            gi[j] = in ? widen(g[place(j)]) : 0.0f;
-            pi[j] = in ? p[place(j)] : 0.0f;
-            cm[j >> 2] |= in ? (uint32_t)m[place(j)] << 8 * (j & 3) : 0u;
-            cv[j >> 2] |= in ? (uint32_t)v[place(j)] << 8 * (j & 3) : 0u;
+            const int at = min(place(j), last);
+            gi[j] = widen(g[at]);
+            pi[j] = p[at];
+            em[j] = m[at];
+            ev[j] = v[at];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = place(j) <= last;
+            gi[j] = in ? gi[j] : 0.0f;
+            cm[j >> 2] |= in ? em[j] << 8 * (j & 3) : 0u;
+            cv[j >> 2] |= in ? ev[j] << 8 * (j & 3) : 0u;
         }
     }
     const StepFactors f = step_factors(k);
-    if (!f.go) return;
+    if (!f.go || !some) return;                              // (the first wavefront, which counts, has elements)
     const Rates r = rates_of(f, k, t);
     // (elements past the layer's end: gradient 0 and codes 0, so their moments are 0)
     decode8(cm, cv, (int)(x & 255u), (int)(x >> 8), mi, vi);
@@ -558,7 +580,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
             }
         }
     }
-    count_step(k, f);                                        // (every workgroup's first thread has elements)
+    count_step(k, f);
 }
 
 // Bound by HBM.  A row of 16 lanes takes a block; for 16-bit values a lane takes 8 consecutive elements, one access of each
@@ -597,11 +619,20 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const CodedPart* __re
             store8(vo, fv);
         }
     } else {
+        uint32_t cm[8], cv[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = min(kRun ? j : place(j), left - 1);
+            cm[j] = m[at];
+            cv[j] = v[at];
+        }
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int at = kRun ? j : place(j);
-            if (at >= left) break;
-            store1(mo + at, decoded_m(m[at], (int)(both & 255u)));
-            store1(vo + at, decoded_v(v[at], (int)(both >> 8)));
+            if (at < left) {
+                store1(mo + at, decoded_m(cm[j], (int)(both & 255u)));
+                store1(vo + at, decoded_v(cv[j], (int)(both >> 8)));
+            }
         }
     }
 }
