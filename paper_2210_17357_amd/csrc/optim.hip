@@ -23,7 +23,10 @@ constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
 // 164; 67 M of bf16: 38, 49, 75 and 130, with 32768 36; 25 M: 22, 24, 30, 47).
 constexpr int kNormPart = 16384, kNormParts = 6000;
 constexpr int kStepPart = 4 * kThreads;        // elements of a workgroup of the step: one access a thread and buffer
-constexpr int kCodedPart = 8 * kThreads;       // the same with 8-bit moments
+// With 8-bit moments a thread takes 8 elements, and workgroups are half as large where short layers would leave more than a quarter
+// of the larger ones idle (us a step, 256 threads / 128: 4000 layers of 200 elements 16.8 / 13.7, 6000 of 1400 38.4 / 36.4; 64 threads:
+// 13.7, 37.  Long layers, a pass of 25 M elements 95.9 / 97.9, of 4.8 M 35.6 / 37.2).
+constexpr int kCodedElems = 8;
 constexpr int kShortParts = 65536;             // most workgroups of a step that works out its own factors
 // Longer steps ask for LDS that they do not use, so that 3 workgroups (5 with 8-bit moments) share a compute unit and not 8: the
 // chip's accesses then stay in a narrower window of memory.  355 M elements, us, with 8 / 6 / 5 / 4 / 3 / 2: fp32 moments
@@ -662,6 +665,7 @@ struct lgreco_optim {
     int32_t L = 0;
     int64_t blocks = 0;
     int64_t n_norm = 0, n_step = 0, n_coded = 0;   // parts of the three cuts of the table
+    int32_t coded_threads = kThreads;              // of the workgroups with 8-bit moments
     uint8_t* d_all = nullptr;                      // one allocation, of
     NormPart* d_norm = nullptr;
     StepPart* d_step = nullptr;                    // cut on whole lines of the flat buffers
@@ -718,9 +722,14 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
         if (parts > 1) norm_words += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
         o->n_norm += parts;
         o->n_step += count_parts(a, kStepPart, kLine);
-        o->n_coded += count_parts(a, kCodedPart, 1);
+        o->n_coded += count_parts(a, kCodedElems * kThreads, 1);
     }
     if (o->n_step > kMaxParts) return LGRECO_ENOSPACE;                      // (the finest of the cuts)
+    if (4 * total < 3 * o->n_coded * kCodedElems * kThreads) {
+        o->coded_threads = kThreads / 2;
+        o->n_coded = 0;
+        for (int32_t l = 0; l < L; ++l) o->n_coded += count_parts(layers[l], kCodedElems * o->coded_threads, 1);
+    }
     o->L = L;
     HIPCHK(hipGetDevice(&o->device));
 
@@ -750,7 +759,7 @@ int create(lgreco_optim* o, const lgreco_layer_t* layers, int32_t L, const float
         });
         if (parts > 1) word += (size_t)kTicketLine * ticket_lines((uint32_t)parts);
         for_parts(layers[l], kStepPart, kLine, [&](int64_t start, int64_t, int64_t n) { *step++ = StepPart{start, (int32_t)n, ls, ds, 0}; });
-        for_parts(layers[l], kCodedPart, 1, [&](int64_t start, int64_t pos, int64_t n) {
+        for_parts(layers[l], kCodedElems * o->coded_threads, 1, [&](int64_t start, int64_t pos, int64_t n) {
             *coded++ = CodedPart{start, (int32_t)n, ls, ds, l, (int32_t)pos, (int32_t)(o->blocks + pos / kOptimBlock)};
         });
         o->blocks += (layers[l].numel + kOptimBlock - 1) / kOptimBlock;
@@ -885,7 +894,7 @@ int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const
         f = grad_type == LGRECO_F32 ? coded_kernel_of<float, true>(d_copy, copy_type) : coded_kernel_of<BF16, true>(d_copy, copy_type);
     else
         f = grad_type == LGRECO_F32 ? coded_kernel_of<float, false>(d_copy, copy_type) : coded_kernel_of<BF16, false>(d_copy, copy_type);
-    HIPCHK(launch(f, o->n_coded, kThreads, k.factors ? kCodedLds : 0, s, k));
+    HIPCHK(launch(f, o->n_coded, o->coded_threads, k.factors ? kCodedLds : 0, s, k));
     return LGRECO_OK;
 }
 
@@ -898,10 +907,10 @@ int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_
     hipStream_t s = (hipStream_t)stream;
     const CodedPart* const parts = o->d_coded;
     if (type == LGRECO_F32)
-        HIPCHK(launch(moments_kernel<float>, o->n_coded, kThreads, 0, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
+        HIPCHK(launch(moments_kernel<float>, o->n_coded, o->coded_threads, 0, s, parts, d_m, d_v, d_exps, static_cast<float*>(d_m_out),
                       static_cast<float*>(d_v_out)));
     else
-        HIPCHK(launch(moments_kernel<BF16>, o->n_coded, kThreads, 0, s, parts, d_m, d_v, d_exps, static_cast<BF16*>(d_m_out),
+        HIPCHK(launch(moments_kernel<BF16>, o->n_coded, o->coded_threads, 0, s, parts, d_m, d_v, d_exps, static_cast<BF16*>(d_m_out),
                       static_cast<BF16*>(d_v_out)));
     return LGRECO_OK;
 }
