@@ -390,12 +390,12 @@ def adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8
 
 class Optim:
     """lgreco_optim_t with the entry points as methods: the optimizer step over the layers of one table.  Tensors have
-    the table's layout (flat, contiguous, on the plan's device, at least `extent` elements)."""
+    the table's layout (flat, contiguous, on the plan's device, at least `extent` elements).  Every GPU method takes `stream`: a
+    HIP stream handle (int); default: torch's current stream of the plan's device."""
 
     def __init__(self, layers, lr_scale: Optional[Sequence[float]] = None, decay_scale: Optional[Sequence[float]] = None):
         import torch
         self._o = C.c_void_p()
-        self._current_stream = torch.cuda.current_stream
         scales = []
         for a in (lr_scale, decay_scale):
             a = None if a is None else np.ascontiguousarray(a, np.float32)
@@ -413,6 +413,13 @@ class Optim:
         self.blocks = int(lib().lgreco_optim_blocks(self._o))
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         self._f32, self._f64, self._u8, self._i64 = torch.float32, torch.float64, torch.uint8, torch.int64
+        # a call is a few microseconds: what it looks up is looked up once (the handle of the current stream without a
+        # Stream object around it, where this torch has that)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current = raw if raw is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
+        l = lib()
+        self._norms, self._adamw, self._coded, self._decode = (l.lgreco_optim_norms, l.lgreco_optim_adamw,
+                                                               l.lgreco_optim_adamw_coded, l.lgreco_optim_decode)
 
     def close(self):
         if self._o:
@@ -425,58 +432,70 @@ class Optim:
         except Exception:
             pass
 
-    def _check(self, st: int):
-        if st != OK:
-            text = strerror(st)
-            if st == EHIP:
-                text += " (" + lib().lgreco_optim_last_hip_error(self._o).decode() + ")"
-            raise LgrecoError(st, text)
+    def _failed(self, st: int):
+        text = strerror(st)
+        if st == EHIP:
+            text += " (" + lib().lgreco_optim_last_hip_error(self._o).decode() + ")"
+        raise LgrecoError(st, text)
 
-    def _ptr(self, t, dtype, numel: int) -> Optional[int]:
-        """Device address of a tensor that has to be of this type (None: one of the floating types a call takes) and size."""
-        if t is None:
-            return None
-        if t.get_device() != self.device or not t.is_contiguous():
+    def _ptr(self, t, dtype, numel: int) -> int:
+        """Device address of a tensor that has to be of this type and size."""
+        if t.dtype is not dtype or t.numel() < numel or t.get_device() != self.device or not t.is_contiguous():
+            if t.dtype is not dtype:
+                raise ValueError("unexpected tensor type %s" % t.dtype)
+            if t.numel() < numel:
+                raise ValueError("the tensor has %d elements, %d are needed" % (t.numel(), numel))
             raise ValueError("expected a contiguous tensor on the plan's device")
-        if t.dtype is not dtype and (dtype is not None or t.dtype not in self._types):
-            raise ValueError("unexpected tensor type %s" % t.dtype)
-        if t.numel() < numel:
-            raise ValueError("the tensor has %d elements, the layers reach to %d" % (t.numel(), numel))
         return t.data_ptr()
 
-    def _stream(self, stream) -> int:
-        return self._current_stream(self.device).cuda_stream if stream is None else int(stream)
+    def _typed(self, t, numel: int):
+        """Device address and type of a tensor of any floating type that calls take."""
+        kind = self._types.get(t.dtype)
+        if kind is None:
+            raise ValueError("unexpected tensor type %s" % t.dtype)
+        return self._ptr(t, t.dtype, numel), kind
 
     def norms(self, d_grads, d_sumsq, stream=None):
         """d_sumsq (fp64, layers + 1): squared norm of every layer's gradient, then of all together."""
-        self._check(lib().lgreco_optim_norms(self._o, self._ptr(d_grads, None, self.extent), self._types[d_grads.dtype],
-                                             self._ptr(d_sumsq, self._f64, self.L + 1), self._stream(stream)))
+        grads, kind = self._typed(d_grads, self.extent)
+        st = self._norms(self._o, grads, kind, self._ptr(d_sumsq, self._f64, self.L + 1),
+                         self._current(self.device) if stream is None else int(stream))
+        if st != OK:
+            self._failed(st)
 
     def adamw(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_step, d_copy=None, d_sumsq=None, d_lr=None, stream=None):
         """One step with fp32 moments; gradients fp32 or bf16, d_copy (bf16 or fp16) receives the parameters too."""
-        n = self.extent
-        self._check(lib().lgreco_optim_adamw(
-            self._o, C.byref(settings), self._ptr(d_grads, None, n), self._types[d_grads.dtype], self._ptr(d_params, self._f32, n),
-            self._ptr(d_m, self._f32, n), self._ptr(d_v, self._f32, n), self._ptr(d_copy, None, n),
-            0 if d_copy is None else self._types[d_copy.dtype], self._ptr(d_sumsq, self._f64, self.L + 1),
-            self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1), self._stream(stream)))
+        n, f32 = self.extent, self._f32
+        grads, kind = self._typed(d_grads, n)
+        copy, copy_kind = (None, 0) if d_copy is None else self._typed(d_copy, n)
+        st = self._adamw(self._o, C.byref(settings), grads, kind, self._ptr(d_params, f32, n), self._ptr(d_m, f32, n),
+                         self._ptr(d_v, f32, n), copy, copy_kind,
+                         None if d_sumsq is None else self._ptr(d_sumsq, self._f64, self.L + 1),
+                         None if d_lr is None else self._ptr(d_lr, f32, 1), self._ptr(d_step, self._i64, 1),
+                         self._current(self.device) if stream is None else int(stream))
+        if st != OK:
+            self._failed(st)
 
     def adamw_coded(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_exps, d_step, d_copy=None, d_sumsq=None, d_lr=None,
                     stream=None):
         """One step with moments in 8 bits: d_m, d_v uint8 codes, d_exps uint8 (2 * blocks) exponents."""
-        n = self.extent
-        self._check(lib().lgreco_optim_adamw_coded(
-            self._o, C.byref(settings), self._ptr(d_grads, None, n), self._types[d_grads.dtype], self._ptr(d_params, self._f32, n),
-            self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
-            self._ptr(d_copy, None, n), 0 if d_copy is None else self._types[d_copy.dtype],
-            self._ptr(d_sumsq, self._f64, self.L + 1), self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1),
-            self._stream(stream)))
+        n, u8 = self.extent, self._u8
+        grads, kind = self._typed(d_grads, n)
+        copy, copy_kind = (None, 0) if d_copy is None else self._typed(d_copy, n)
+        st = self._coded(self._o, C.byref(settings), grads, kind, self._ptr(d_params, self._f32, n), self._ptr(d_m, u8, n),
+                         self._ptr(d_v, u8, n), self._ptr(d_exps, u8, 2 * self.blocks), copy, copy_kind,
+                         None if d_sumsq is None else self._ptr(d_sumsq, self._f64, self.L + 1),
+                         None if d_lr is None else self._ptr(d_lr, self._f32, 1), self._ptr(d_step, self._i64, 1),
+                         self._current(self.device) if stream is None else int(stream))
+        if st != OK:
+            self._failed(st)
 
     def decode(self, d_m, d_v, d_exps, d_m_out, d_v_out, stream=None):
         """Values of 8-bit moments, both outputs fp32 or both bf16."""
-        n = self.extent
-        if d_m_out.dtype is not d_v_out.dtype:
-            raise ValueError("outputs of one type")
-        self._check(lib().lgreco_optim_decode(
-            self._o, self._ptr(d_m, self._u8, n), self._ptr(d_v, self._u8, n), self._ptr(d_exps, self._u8, 2 * self.blocks),
-            self._ptr(d_m_out, None, n), self._ptr(d_v_out, None, n), self._types[d_m_out.dtype], self._stream(stream)))
+        n, u8 = self.extent, self._u8
+        m_out, kind = self._typed(d_m_out, n)
+        st = self._decode(self._o, self._ptr(d_m, u8, n), self._ptr(d_v, u8, n), self._ptr(d_exps, u8, 2 * self.blocks), m_out,
+                          self._ptr(d_v_out, d_m_out.dtype, n), kind,
+                          self._current(self.device) if stream is None else int(stream))
+        if st != OK:
+            self._failed(st)
