@@ -386,8 +386,8 @@ __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, fl
     p -= __builtin_fmaf(r.shrink, p, r.rate * u);
 }
 
-// Bound by HBM, four streams in and three or four out.  A thread takes 4 elements and is done: 355 M elements in 1648 us
-// (28 bytes each: 6.0 TB/s).  With 8 workgroups a compute unit 1725, then 1810 with two rounds a workgroup, 1870 with eight, 1830 with
+// Bound by HBM, four streams in and three or four out.  A thread takes 4 elements and is done: 355 M elements in 1635 us
+// (28 bytes each: 6.1 TB/s).  With 8 workgroups a compute unit 1725, then 1810 with two rounds a workgroup, 1870 with eight, 1830 with
 // both rounds' loads ahead, 1955 without the streaming hints.
 template <typename G, typename C>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepParams k) {
@@ -490,7 +490,7 @@ __device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t 
     }
 }
 
-// Bound by HBM: 355 M elements with bf16 gradients and copy, stochastic, in 940 us (16 bytes each: 6.0 TB/s); rounding to nearest
+// Bound by HBM: 355 M elements with bf16 gradients and copy, stochastic, in 932 us (16 bytes each: 6.1 TB/s); rounding to nearest
 // takes as long.  A row of 16 lanes takes a block, so that its maxima take four vector instructions each and no LDS.  (Lanes with 8
 // consecutive elements, whose fp32 accesses are half lines: 1100; the codes' accesses with streaming hints: 1 to 3 % more.)
 template <typename G, typename C, bool STOCHASTIC>
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
 }
 
 // Bound by HBM.  A row of 16 lanes takes a block; for 16-bit values a lane takes 8 consecutive elements, one access of each
-// buffer (355 M elements: 365 us, 5.8 TB/s, 390 as for fp32).
+// buffer (355 M elements: 360 us, 5.9 TB/s, 390 as for fp32).
 template <typename O>
 __global__ __launch_bounds__(kThreads) void moments_kernel(const CodedPart* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
