@@ -438,7 +438,7 @@ int lgreco_optim_destroy(lgreco_optim_t* o);
 int64_t lgreco_optim_blocks(const lgreco_optim_t* o);
 
 /* Squared norms of the gradients as they are (before any grad_scale).
- *   grad_type  LGRECO_F32 or LGRECO_BF16
+ *   grad_type  LGRECO_F32, LGRECO_BF16 or LGRECO_F16
  *   d_sumsq    device out [L + 1], fp64: [l] sum of the squares of layer l, [L] sum over all layers.  Summed in
  *              fp64 in an order that only depends on the table: two calls give the same bits.  A NaN or an
  *              infinity among the gradients makes the layer's sum and the last one NaN or infinite. */
@@ -450,7 +450,7 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
  *   p' = p - lr_l wd_l p - lr_l / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
  * in fp32, the factors that are the same for all elements in fp64.  Of m' and v' every factor, product and sum is
  * rounded to fp32 (c as well), so that they are reproducible bit for bit: v' = beta2 * v + (1 - beta2) * (g * g).
- *   grad_type  LGRECO_F32 or LGRECO_BF16
+ *   grad_type  LGRECO_F32, LGRECO_BF16 or LGRECO_F16
  *   d_params   fp32, in/out;   d_m, d_v  fp32 moments, in/out (zero before the first step)
  *   d_copy     out: p' rounded to nearest even in copy_type (LGRECO_BF16 or LGRECO_F16; fp16: beyond
  *              65504 infinite), or NULL

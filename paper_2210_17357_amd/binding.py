@@ -464,7 +464,7 @@ class Optim:
             self._failed(st)
 
     def adamw(self, settings: AdamW, d_grads, d_params, d_m, d_v, d_step, d_copy=None, d_sumsq=None, d_lr=None, stream=None):
-        """One step with fp32 moments; gradients fp32 or bf16, d_copy (bf16 or fp16) receives the parameters too."""
+        """One step with fp32 moments; gradients fp32, bf16 or fp16, d_copy (bf16 or fp16) receives the parameters too."""
         n, f32 = self.extent, self._f32
         grads, kind = self._typed(d_grads, n)
         copy, copy_kind = (None, 0) if d_copy is None else self._typed(d_copy, n)

@@ -85,6 +85,7 @@ struct NoCopy { };
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(BF16 x) { return __builtin_bit_cast(float, (uint32_t)x.bits << 16); }
+__device__ __forceinline__ float widen(F16 x) { return (float)__builtin_bit_cast(_Float16, x.bits); }
 __device__ __forceinline__ uint16_t narrow_bits(float x, BF16) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t narrow_bits(float x, F16) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 
@@ -92,19 +93,21 @@ __device__ __forceinline__ void load4(const float* p, float* x) {
     const float4 v = load_stream(p);
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
-__device__ __forceinline__ void load4(const BF16* p, float* x) {
+template <typename G>
+__device__ __forceinline__ void load4(const G* p, float* x) {
     const u16x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = widen(BF16{v[j]});
+    for (int j = 0; j < 4; ++j) x[j] = widen(G{v[j]});
 }
 // one 16-byte access
 __device__ __forceinline__ void load16(const float* p, float (&x)[4]) { load4(p, x); }
-__device__ __forceinline__ void load16(const BF16* p, float (&x)[8]) {
+template <typename G>
+__device__ __forceinline__ void load16(const G* p, float (&x)[8]) {
     const u32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __builtin_bit_cast(float, v[j] << 16);
-        x[2 * j + 1] = __builtin_bit_cast(float, v[j] & 0xFFFF0000u);
+        x[2 * j] = widen(G{(uint16_t)v[j]});
+        x[2 * j + 1] = widen(G{(uint16_t)(v[j] >> 16)});
     }
 }
 template <typename C>
@@ -653,6 +656,7 @@ hipError_t launch(void (*kernel)(A...), int64_t grid, int threads, size_t lds, h
 }
 
 size_t element_size(int32_t type) { return type == LGRECO_F32 ? 4 : 2; }
+bool gradient_type(int32_t type) { return type == LGRECO_F32 || type == LGRECO_BF16 || type == LGRECO_F16; }
 bool misaligned(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
 
 }  // namespace
@@ -794,7 +798,7 @@ int begin_step(lgreco_optim* o, const lgreco_adamw_t* c, const void* grads, int3
                const void* v, size_t moment_size, const void* copy, int32_t copy_type, const double* sumsq, const float* lr,
                int64_t* step, hipStream_t s, const void* parts, int64_t n_parts, StepParams* k) {
     if (!c || !grads || !params || !m || !v || !step || !valid(c)) return LGRECO_EINVAL;
-    if (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16) return LGRECO_EINVAL;
+    if (!gradient_type(grad_type)) return LGRECO_EINVAL;
     if (copy && copy_type != LGRECO_BF16 && copy_type != LGRECO_F16) return LGRECO_EINVAL;
     if (c->max_norm > 0.0 && !sumsq) return LGRECO_EINVAL;
     if (misaligned(grads, element_size(grad_type)) || misaligned(params, 4) || misaligned(m, moment_size) ||
@@ -821,6 +825,10 @@ template <typename G, bool STOCHASTIC>
 StepKernel coded_kernel_of(bool copy, int32_t copy_type) {
     return !copy ? adamw_coded_kernel<G, NoCopy, STOCHASTIC>
                  : copy_type == LGRECO_BF16 ? adamw_coded_kernel<G, BF16, STOCHASTIC> : adamw_coded_kernel<G, F16, STOCHASTIC>;
+}
+template <typename G>
+StepKernel coded_kernel_of(bool stochastic, bool copy, int32_t copy_type) {
+    return stochastic ? coded_kernel_of<G, true>(copy, copy_type) : coded_kernel_of<G, false>(copy, copy_type);
 }
 
 }  // namespace
@@ -856,13 +864,14 @@ int64_t lgreco_optim_blocks(const lgreco_optim_t* o) { return o ? o->blocks : -1
 const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o) { return o ? o->error : ""; }
 
 int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type, double* d_sumsq, void* stream) {
-    if (!o || !d_grads || !d_sumsq || (grad_type != LGRECO_F32 && grad_type != LGRECO_BF16)) return LGRECO_EINVAL;
+    if (!o || !d_grads || !d_sumsq || !gradient_type(grad_type)) return LGRECO_EINVAL;
     if (misaligned(d_grads, element_size(grad_type)) || misaligned(d_sumsq, 8)) return LGRECO_EINVAL;
     const int st = on_device(o);
     if (st != LGRECO_OK) return st;
     hipStream_t s = (hipStream_t)stream;
     const NormParams k{o->d_norm, d_grads, o->d_partials, d_sumsq, o->L, o->d_norm_tickets};
-    HIPCHK(launch(grad_type == LGRECO_F32 ? norms_kernel<float> : norms_kernel<BF16>, o->n_norm, kThreads, 0, s, k));
+    HIPCHK(launch(grad_type == LGRECO_F32 ? norms_kernel<float> : grad_type == LGRECO_BF16 ? norms_kernel<BF16> : norms_kernel<F16>, o->n_norm,
+                  kThreads, 0, s, k));
     return LGRECO_OK;
 }
 
@@ -874,7 +883,8 @@ int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void*
     StepParams k;
     const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 4, d_copy, copy_type, d_sumsq, d_lr, d_step, s, o->d_step, o->n_step, &k);
     if (st != LGRECO_OK) return st;
-    const StepKernel f = grad_type == LGRECO_F32 ? adamw_kernel_of<float>(d_copy, copy_type) : adamw_kernel_of<BF16>(d_copy, copy_type);
+    const StepKernel f = grad_type == LGRECO_F32    ? adamw_kernel_of<float>(d_copy, copy_type)
+                         : grad_type == LGRECO_BF16 ? adamw_kernel_of<BF16>(d_copy, copy_type) : adamw_kernel_of<F16>(d_copy, copy_type);
     HIPCHK(launch(f, o->n_step, kThreads, k.factors ? kStepLds : 0, s, k));
     return LGRECO_OK;
 }
@@ -889,11 +899,10 @@ int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const
     const int st = begin_step(o, cfg, d_grads, grad_type, d_params, d_m, d_v, 1, d_copy, copy_type, d_sumsq, d_lr, d_step, s, o->d_coded, o->n_coded, &k);
     if (st != LGRECO_OK) return st;
     k.exps = d_exps;
-    StepKernel f;
-    if (cfg->stochastic)
-        f = grad_type == LGRECO_F32 ? coded_kernel_of<float, true>(d_copy, copy_type) : coded_kernel_of<BF16, true>(d_copy, copy_type);
-    else
-        f = grad_type == LGRECO_F32 ? coded_kernel_of<float, false>(d_copy, copy_type) : coded_kernel_of<BF16, false>(d_copy, copy_type);
+    const bool random = cfg->stochastic != 0;
+    const StepKernel f = grad_type == LGRECO_F32    ? coded_kernel_of<float>(random, d_copy, copy_type)
+                         : grad_type == LGRECO_BF16 ? coded_kernel_of<BF16>(random, d_copy, copy_type)
+                                                    : coded_kernel_of<F16>(random, d_copy, copy_type);
     HIPCHK(launch(f, o->n_coded, o->coded_threads, k.factors ? kCodedLds : 0, s, k));
     return LGRECO_OK;
 }

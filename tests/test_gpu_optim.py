@@ -101,7 +101,7 @@ def rounded16(x, kind):
 
 # ------------------------------------------------------------------------------ norms
 @pytest.mark.parametrize("name", sorted(TABLES))
-@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 def test_norms(name, kind):
     from paper_2210_17357_amd import binding as B
     torch = torch_cuda()
@@ -153,7 +153,7 @@ def test_norms_of_extreme_values():
 
 # ------------------------------------------------------------------------------ fp32 moments
 @pytest.mark.parametrize("name", sorted(TABLES))
-@pytest.mark.parametrize("kind,copy", list(itertools.product(("f32", "bf16"), TYPES)))
+@pytest.mark.parametrize("kind,copy", list(itertools.product(("f32", "bf16", "f16"), TYPES)))
 def test_adamw(name, kind, copy):
     from paper_2210_17357_amd import binding as B
     torch = torch_cuda()
@@ -330,7 +330,9 @@ def check_coded(new, tol, codes_m, codes_v, exps, u):
 @pytest.mark.parametrize("kind,copy,stochastic", [("f32", "none", False), ("f32", "none", True), ("bf16", "bf16", True),
                                                   ("bf16", "f16", False), ("f32", "f16", True), ("f32", "bf16", False),
                                                   ("bf16", "none", True), ("bf16", "none", False), ("f32", "bf16", True),
-                                                  ("bf16", "f16", True), ("bf16", "bf16", False), ("f32", "f16", False)])
+                                                  ("bf16", "f16", True), ("bf16", "bf16", False), ("f32", "f16", False),
+                                                  ("f16", "none", True), ("f16", "f16", False), ("f16", "bf16", True),
+                                                  ("f16", "none", False), ("f16", "f16", True), ("f16", "bf16", False)])
 def test_adamw_coded(name, kind, copy, stochastic):
     """Three steps from zero moments: parameters, codes and exponents of each against the step in 64 bits from what the
     one before left."""
@@ -815,10 +817,6 @@ def test_refusals():
         with pytest.raises(B.LgrecoError):
             plan.adamw(s, f32(), f32(), f32(), f32(), step)
     half = torch.zeros(700, dtype=torch.float16, device="cuda")
-    with pytest.raises(B.LgrecoError):                  # fp16 gradients
-        plan.norms(half, sums)
-    with pytest.raises(B.LgrecoError):
-        plan.adamw(good, half, f32(), f32(), f32(), step)
     with pytest.raises(B.LgrecoError):                  # an fp32 copy
         plan.adamw(good, f32(), f32(), f32(), f32(), step, d_copy=f32())
     with pytest.raises(B.LgrecoError):                  # values in fp16
