@@ -733,6 +733,78 @@ def test_receive_is_the_sum_of_the_workers_and_a_step(coded, max_norm):
         assert torch.equal(run.d_copy, run.d_params.to(torch.bfloat16))
 
 
+def test_the_largest_layer():
+    """One layer of 2^31 - 1 elements: pieces of it, the last one among them, against plans of those pieces."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    n = 2 ** 31 - 1
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    g = torch.empty(n, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    p = torch.ones(n, device="cuda")
+    plan = B.Optim(table(B, [0], [n]))
+    sums = torch.zeros(2, dtype=torch.float64, device="cuda")
+    plan.norms(g, sums)
+    want = sum(float(part.double().square().sum()) for part in g.split(1 << 28))
+    assert np.allclose(sums.cpu().numpy(), want, rtol=1e-12, atol=0)
+    s = B.adamw(lr=1e-2, max_norm=1e5)
+    pieces = [(0, 5000), (2 ** 30 - 128, 4096), (n - n % 128 - 1280, 1280 + n % 128)]
+    for coded in (False, True):
+        kind = torch.uint8 if coded else torch.float32
+        st = [p.clone(), torch.zeros(n, dtype=kind, device="cuda"), torch.zeros(n, dtype=kind, device="cuda")]
+        st += [torch.zeros(2 * plan.blocks, dtype=torch.uint8, device="cuda")] if coded else []
+        step = torch.zeros(1, dtype=torch.int64, device="cuda")
+        (plan.adamw_coded if coded else plan.adamw)(s, g, *st, step, d_sumsq=sums)
+        assert int(step) == 1
+        for o, k in pieces:
+            few = B.Optim(table(B, [0], [k]))
+            part = [p[o:o + k].clone(), torch.zeros(k, dtype=kind, device="cuda"), torch.zeros(k, dtype=kind, device="cuda")]
+            part += [torch.zeros(2 * few.blocks, dtype=torch.uint8, device="cuda")] if coded else []
+            (few.adamw_coded if coded else few.adamw)(s, g[o:o + k].clone(), *part, torch.zeros(1, dtype=torch.int64, device="cuda"), d_sumsq=sums)
+            # (a piece that ends inside a block of the layer has a block of its own there: whole blocks are compared)
+            whole = k if not coded or o + k == n else k // 128 * 128
+            for a, b in zip(st[:3], part[:3]):
+                assert torch.equal(a[o:o + whole], b[:whole]), (coded, o)
+            if coded:
+                blocks = (whole + 127) // 128
+                assert torch.equal(st[3][2 * (o // 128):2 * (o // 128) + 2 * blocks], part[3][:2 * blocks]), o
+        del st
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_layers_in_any_order_and_two_plans_at_once(coded):
+    """A table that lists the layers from the last to the first, and two plans stepping their halves of the buffers on two
+    streams at once: the same parameters and moments as one plan in order."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout([70000, 129, 33333, 1, 4096, 50001], 1, 2)
+    g, p, _, _ = values(np.random.default_rng(19), n, offs, numels)
+    dg, kind = torch.from_numpy(g).cuda(), torch.uint8 if coded else torch.float32
+    s = B.adamw(lr=1e-2)
+    results = []
+    for cuts in ([[0, 1, 2, 3, 4, 5]], [[5, 4, 3, 2, 1, 0]], [[0, 2, 4], [5, 3, 1]]):
+        d = [torch.from_numpy(p).cuda(), torch.zeros(n, dtype=kind, device="cuda"), torch.zeros(n, dtype=kind, device="cuda")]
+        plans = [B.Optim(table(B, offs[c], numels[c])) for c in cuts]
+        streams = [torch.cuda.Stream() for _ in cuts]
+        exps = [torch.zeros(2 * q.blocks, dtype=torch.uint8, device="cuda") for q in plans]
+        steps = [torch.zeros(1, dtype=torch.int64, device="cuda") for _ in cuts]
+        sums = [torch.zeros(q.L + 1, dtype=torch.float64, device="cuda") for q in plans]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for q, stream, x, k, z in zip(plans, streams, exps, steps, sums):
+                q.norms(dg, z, stream=stream.cuda_stream)
+                if coded:
+                    q.adamw_coded(s, dg, *d, x, k, d_sumsq=z, stream=stream.cuda_stream)
+                else:
+                    q.adamw(s, dg, *d, k, d_sumsq=z, stream=stream.cuda_stream)
+        torch.cuda.synchronize()
+        assert all(int(k) == 20 for k in steps)
+        by_layer = {l: float(z[j]) for c, z in zip(cuts, sums) for j, l in enumerate(c)}
+        results.append(d + [torch.tensor([by_layer[l] for l in range(6)], dtype=torch.float64)])
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("coded", [False, True])
 def test_captured_steps_of_a_long_table(coded):
     """The same for a table beyond 65536 workgroups, against eager steps of another plan."""
