@@ -370,22 +370,25 @@ struct Rates {
     float shrink;        // lr wd
     float rate;          // lr / (1 - b1^t)
     float grad, root_v;
+    float root_low;      // root_v behind the root of a v scaled by 2^64
 };
 template <typename P>
 __device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams& p, const P& t) {
     const double s = (double)t.lr_scale;
-    return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v};
+    return Rates{(float)(f.lr * s * (p.weight_decay * (double)t.decay_scale)), (float)(f.lr_m * s), f.grad, f.root_v, f.root_v * 0x1p-32f};
 }
 
 // The moments' products and sums are rounded one by one, so that they, and the codes made of them, are what any other fp32
 // program finds (a fused product moves one code in some ten million to its neighbour).
 // The root and the reciprocal are the instructions' (one unit in the last place), which take 8 cycles where the correctly
-// rounded ones take some 50.  (A v below 2^-126 may count as 0 in the denominator; eps is a normal number.)
+// rounded ones take some 50.  The root's takes numbers below 2^-126 for 0: such a v is scaled by 2^64 under it, exactly.
 __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, float grad, float& p, float& m, float& v) {
     const float g = r.grad * grad;
     m = k.beta1 * m + k.rest1 * g;
     v = k.beta2 * v + k.rest2 * (g * g);
-    const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), r.root_v, k.eps));
+    const bool low = v < FLT_MIN;
+    const float root = __builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v);
+    const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(root, low ? r.root_low : r.root_v, k.eps));
     p -= __builtin_fmaf(r.shrink, p, r.rate * u);
 }
 

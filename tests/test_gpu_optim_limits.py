@@ -1,0 +1,77 @@
+"""GPU: the optimizer step at the limits of what it takes, for both forms of moments."""
+import numpy as np
+import pytest
+
+from oracle import optim as O
+
+from gpu_util import torch_cuda
+from test_gpu_optim import B1, B2, EPS, TABLES, U, bounds, exact_grads, layout, near, stored, table, typed
+
+pytestmark = pytest.mark.gpu
+TINY = 2.0 ** -148                                      # two of the smallest steps of fp32, each off by half
+
+
+def fresh(torch, plan, n, coded):
+    """Zero moments of either form, exponents among them."""
+    kind = torch.uint8 if coded else torch.float32
+    st = [torch.zeros(n, dtype=kind, device="cuda") for _ in range(2)]
+    return st + ([torch.zeros(2 * plan.blocks, dtype=torch.uint8, device="cuda")] if coded else [])
+
+
+def step_of(plan, coded):
+    return plan.adamw_coded if coded else plan.adamw
+
+
+def held(st, offs, numels, coded):
+    """The moments that a state holds, in fp64."""
+    a = [x.cpu().numpy() for x in st]
+    if not coded:
+        return [x.astype(np.float64) for x in a]
+    m, v, first, exps = np.zeros(a[0].size), np.zeros(a[0].size), 0, a[2].reshape(-1, 2)
+    for o, k in zip(offs, numels):
+        c, b = slice(o, o + k), slice(first, first + (k + 127) // 128)
+        m[c], v[c] = stored(a[0][c], exps[b, 0], O.OCTAVES_M, True), stored(a[1][c], exps[b, 1], O.OCTAVES_V, False)
+        first = b.stop
+    return [m, v]
+
+
+def small_bounds(g, p, m, v, t, lr, beta2, eps):
+    """p' in fp64 and what the step in fp32 may be off it where v' may lie below the smallest normal number: v' is off by its
+    roundings, absolute ones there; the root by what that makes of it and one unit (2 u), the factor, the eps, their sum
+    and the second rounding of the factor's product by u each; reciprocal 2 u, products and the rate 4 u."""
+    new = O.step(g, p, m, v, t, lr, B1, beta2, eps, 0.0, 1.0)
+    a = np.abs(new[1])
+    em = 6 * U * (np.abs(B1 * m) + (1 - B1) * np.abs(g)) + TINY
+    ev = 9 * U * new[2] + TINY
+    root = 1 / np.sqrt(1 - beta2 ** t)
+    side = [np.sqrt(np.maximum(new[2] + e, 0)) * root for e in (-ev, 0.0, ev)]
+    den = side[1] + eps
+    off = np.maximum(side[2] - side[1], side[1] - side[0]) + 6 * U * den
+    assert (off < den).all()
+    rate = lr / (1 - B1 ** t)
+    return new[0], rate * ((a + em) / (den - off) * (1 + 8 * U) - a / den) + U * np.abs(new[0]) + TINY
+
+
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("beta2,eps,smallest", [(0.999, 1e-20, 1e-20), (0.999, 1e-30, 1e-20), (0.999, 1.2e-38, 1e-20), (0.5, 1e-25, 1e-21),
+                                                (1 - 1e-7, 1e-16, 1e-17), (1 - 1e-7, 1e-30, 1e-17)])
+def test_small_eps(beta2, eps, smallest, coded):
+    """Gradients whose squares lie at and below the smallest normal number, under an eps that does not hide their root: three
+    steps from zero moments, each against the formula from what the one before left."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout(*TABLES["blocks"])
+    rng = np.random.default_rng(21)
+    inside = np.zeros(n, bool)
+    for o, k in zip(offs, numels):
+        inside[o:o + k] = True
+    plan = B.Optim(table(B, offs, numels))
+    st, dp, step = fresh(torch, plan, n, coded), torch.zeros(n, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    s = B.adamw(lr=1e-3, beta1=B1, beta2=beta2, eps=eps, weight_decay=0.0)
+    for t in (1, 2, 3):
+        g = (smallest * 10.0 ** rng.uniform(0, 4, n) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+        p, (m, v) = dp.cpu().numpy(), held(st, offs, numels, coded)
+        step_of(plan, coded)(s, torch.from_numpy(g).cuda(), dp, *st, step)
+        want, tol = small_bounds(g[inside], p[inside], m[inside], v[inside], t, 1e-3, beta2, eps)
+        near(dp.cpu().numpy()[inside], want, tol, ("p", t))
+    assert int(step) == 3
