@@ -455,8 +455,9 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
  *   d_copy     out: p' rounded to nearest even in copy_type (LGRECO_BF16 or LGRECO_F16; fp16: beyond
  *              65504 infinite), or NULL
  *   d_sumsq    the array lgreco_optim_norms filled (or the same summed over shards), or NULL.  When S is
- *              NaN or infinite, the step is left out: no buffer and no step count changes.
- *              Required with max_norm > 0.
+ *              NaN or infinite, or c * sqrt(S) exceeds 2^63.5 (about 1.3e19, where squares of g near the end of
+ *              fp32), the step is left out: no buffer and no step count changes.  Without it a |g| from 2^64 on
+ *              makes its v infinite for good.  Required with max_norm > 0.
  *   d_lr       fp32 on the device, multiplies lr (a schedule that replays follow), or NULL (= 1)
  *   d_step     int64 on the device: steps taken so far (>= 0), in/out */
 int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
@@ -477,7 +478,8 @@ int lgreco_optim_adamw(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void*
  * beta2 = 0.999 it hardly ever falls.  Stochastic rounding is free of that: up with the probability that keeps the
  * expectation, from word (i mod 4) of Philox4x32-10 keyed by seed at the counter (i / 4, t, l, 1) (t modulo 2^32, its upper
  * half added to the 1), i the element's index within layer l; m takes the lower 16 bits, v the upper ones.
- * NaN or infinite gradients, where d_sumsq is not there to leave the step out, give undefined moments in their blocks (never a fault). */
+ * Gradients that are NaN or infinite, or a |g| from 2^63.5 on, where d_sumsq is not there to leave the step out, give undefined moments
+ * in their blocks (never a fault). */
 int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const void* d_grads, int32_t grad_type,
                              float* d_params, uint8_t* d_m, uint8_t* d_v, uint8_t* d_exps, void* d_copy,
                              int32_t copy_type, const double* d_sumsq, const float* d_lr, int64_t* d_step,

@@ -72,6 +72,7 @@ struct StepFactors {
     int32_t pad;
 };
 constexpr int kFactorWords = sizeof(StepFactors) / 4;
+constexpr double kMaxNorm = 0x1.6a09e667f3bcdp63;   // 2^63.5: squares up to half of what fp32 holds
 
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
@@ -287,8 +288,11 @@ __device__ __forceinline__ StepFactors factors_of(const FactorParams& p) {
     const uint64_t t = (uint64_t)(*p.step + 1);
     StepFactors f{};
     double c = p.grad_scale;
-    f.go = s <= DBL_MAX;                                         // neither NaN nor infinite
-    if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * sqrt(s) + 1e-6));
+    const double norm = sqrt(s);
+    if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * norm + 1e-6));
+    // neither NaN nor infinite, and no square of a scaled gradient beyond fp32: one would make its v infinite for good, and
+    // with it the exponent of its block
+    f.go = s <= DBL_MAX && c * norm <= kMaxNorm;
     // b^t by squaring: its relative error is some t 2^-53, and b^t is 0 long before that matters
     double power1 = 1.0, power2 = 1.0, b1 = p.beta1, b2 = p.beta2;
     for (uint64_t n = t; n; n >>= 1) {

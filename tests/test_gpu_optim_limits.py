@@ -75,3 +75,34 @@ def test_small_eps(beta2, eps, smallest, coded):
         want, tol = small_bounds(g[inside], p[inside], m[inside], v[inside], t, 1e-3, beta2, eps)
         near(dp.cpu().numpy()[inside], want, tol, ("p", t))
     assert int(step) == 3
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_gradients_whose_squares_leave_fp32(coded):
+    """With the sums a step of finite gradients whose squares do not fit fp32 is left out, as one of gradients that are not
+    finite is; at the limit, behind a factor, and clipped it is taken."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout([700, 3000], 0, 0)
+    rng = np.random.default_rng(22)
+    p = rng.standard_normal(n).astype(np.float32)
+    plan = B.Optim(table(B, offs, numels))
+    for peak, scale, max_norm, taken in ((3e19, 1.0, 0.0, False), (-3e38, 1.0, 0.0, False), (1.31e19, 1.0, 0.0, False), (1.3e19, 1.0, 0.0, True),
+                                         (3e19, 0.25, 0.0, True), (3e19, 4.0, 1.0, True), (-3e38, 1.0, 10.0, True), (3e19, 4.0, 1e30, False)):
+        g = (rng.standard_normal(n) * 1e-3).astype(np.float32)
+        g[3000] = peak
+        dg, sums = torch.from_numpy(g).cuda(), torch.zeros(3, dtype=torch.float64, device="cuda")
+        plan.norms(dg, sums)
+        c = O.clip(float((g[:3700].astype(np.float64) ** 2).sum()), scale, max_norm)
+        assert (c * abs(peak) < 2 ** 63.5) == taken
+        st = [torch.from_numpy(p).cuda()] + fresh(torch, plan, n, coded)
+        old, step = [a.clone() for a in st], torch.zeros(1, dtype=torch.int64, device="cuda")
+        step_of(plan, coded)(B.adamw(lr=1e-3, beta1=B1, beta2=B2, eps=EPS, weight_decay=0.0, grad_scale=scale, max_norm=max_norm), dg,
+                             *st, step, d_sumsq=sums)
+        assert int(step) == taken, peak
+        if not taken:
+            assert all(torch.equal(a, b) for a, b in zip(old, st)), peak
+            continue
+        new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1e-3, 0.0, c)
+        near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], ("p", peak))
+        assert all(np.isfinite(a).all() for a in held(st[1:], offs, numels, coded))
