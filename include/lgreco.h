@@ -419,7 +419,7 @@ typedef struct {
     double   eps;           /* positive and a normal number as fp32 */
     double   weight_decay;  /* >= 0 */
     double   grad_scale;    /* every gradient is multiplied by it first: 1 / workers behind a sum of their
-                             * gradients, 1 / loss scale; > 0 */
+                             * gradients, 1 / loss scale; positive and a normal number as fp32 */
     double   max_norm;      /* > 0: gradients are clipped to this global norm (after grad_scale); 0: not */
     uint64_t seed;          /* of the stochastic rounding */
     int32_t  stochastic;    /* 8-bit moments: 0 round to nearest, ties to even codes; 1 stochastically */
@@ -456,7 +456,8 @@ int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type
  *              65504 infinite), or NULL
  *   d_sumsq    the array lgreco_optim_norms filled (or the same summed over shards), or NULL.  When S is
  *              NaN or infinite, or c * sqrt(S) exceeds 2^63.5 (about 1.3e19, where squares of g near the end of
- *              fp32), the step is left out: no buffer and no step count changes.  Without it a |g| from 2^64 on
+ *              fp32), or clipping takes c below 2^-126 (where fp32 holds it with a few bits or as 0), the step is
+ *              left out: no buffer and no step count changes.  Without it a |g| from 2^64 on
  *              makes its v infinite for good.  Required with max_norm > 0.
  *   d_lr       fp32 on the device, multiplies lr (a schedule that replays follow), or NULL (= 1)
  *   d_step     int64 on the device: steps taken so far (>= 0), in/out */

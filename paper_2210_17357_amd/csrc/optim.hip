@@ -291,8 +291,8 @@ __device__ __forceinline__ StepFactors factors_of(const FactorParams& p) {
     const double norm = sqrt(s);
     if (p.max_norm > 0.0) c *= fmin(1.0, p.max_norm / (p.grad_scale * norm + 1e-6));
     // neither NaN nor infinite, and no square of a scaled gradient beyond fp32: one would make its v infinite for good, and
-    // with it the exponent of its block
-    f.go = s <= DBL_MAX && c * norm <= kMaxNorm;
+    // with it the exponent of its block; a factor below the normal numbers would round the gradients to a few bits or to 0
+    f.go = s <= DBL_MAX && c * norm <= kMaxNorm && c >= FLT_MIN;
     // b^t by squaring: its relative error is some t 2^-53, and b^t is 0 long before that matters
     double power1 = 1.0, power2 = 1.0, b1 = p.beta1, b2 = p.beta2;
     for (uint64_t n = t; n; n >>= 1) {
@@ -796,8 +796,8 @@ int on_device(lgreco_optim* o) {
 bool valid(const lgreco_adamw_t* c) {
     const auto finite_from = [](double x, double least) { return x >= least && x <= DBL_MAX; };
     return finite_from(c->lr, 0.0) && c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0 &&
-           c->eps <= FLT_MAX && (float)c->eps >= FLT_MIN && finite_from(c->weight_decay, 0.0) && c->grad_scale > 0.0 &&
-           c->grad_scale <= DBL_MAX && finite_from(c->max_norm, 0.0) && (c->stochastic == 0 || c->stochastic == 1) && c->reserved == 0;
+           c->eps <= FLT_MAX && (float)c->eps >= FLT_MIN && finite_from(c->weight_decay, 0.0) && c->grad_scale >= FLT_MIN &&
+           c->grad_scale <= FLT_MAX && finite_from(c->max_norm, 0.0) && (c->stochastic == 0 || c->stochastic == 1) && c->reserved == 0;
 }
 
 // What both forms of the step check and queue in front of their kernel.

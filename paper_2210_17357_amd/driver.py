@@ -63,7 +63,7 @@ class AdamW:
     """Parameters' update behind the exchange: moments (fp32, or 8 bits with `coded`), step count and norms of the
     layers of one flat parameter buffer.  `layers` are all the tensors to be stepped, also those that travel
     uncompressed.  With `guard` (always with clipping) a step whose gradients are not finite, or too large for their squares
-    in fp32, is left out.
+    or for clipping's factor in fp32, is left out.
     Nothing waits for the GPU in `step`; it may be captured into a HIP graph.  The state is made and read out on torch's
     current stream: a caller whose steps run on another one orders the two."""
 

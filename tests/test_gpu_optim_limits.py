@@ -106,3 +106,43 @@ def test_gradients_whose_squares_leave_fp32(coded):
         new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1e-3, 0.0, c)
         near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], ("p", peak))
         assert all(np.isfinite(a).all() for a in held(st[1:], offs, numels, coded))
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_the_gradients_factor_is_a_normal_number(coded):
+    """Factors that fp32 holds as infinite, as 0 or with a few bits only are refused, and a clipped step that comes to one is left out."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout([700, 3000], 0, 0)
+    rng = np.random.default_rng(23)
+    p = rng.standard_normal(n).astype(np.float32)
+    plan = B.Optim(table(B, offs, numels))
+    f = step_of(plan, coded)
+    least, most = 2.0 ** -126, float(np.finfo(np.float32).max)
+    zero = torch.zeros(n, device="cuda")
+    for scale in (1e39, 1e300, least * 0.99, 1e-42, 1e-60, 1e-300):
+        st, step = [torch.from_numpy(p).cuda()] + fresh(torch, plan, n, coded), torch.zeros(1, dtype=torch.int64, device="cuda")
+        with pytest.raises(B.LgrecoError) as e:
+            f(B.adamw(lr=1e-3, grad_scale=scale), zero, *st, step)
+        assert e.value.status == B.EINVAL
+    for scale, size in ((least, 1e37), (most, 1e-38)):
+        g = (rng.standard_normal(n) * size).astype(np.float32)
+        st, step = [torch.from_numpy(p).cuda()] + fresh(torch, plan, n, coded), torch.zeros(1, dtype=torch.int64, device="cuda")
+        f(B.adamw(lr=1e-3, beta1=B1, beta2=B2, eps=EPS, weight_decay=0.0, grad_scale=scale), torch.from_numpy(g).cuda(), *st, step)
+        new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1e-3, 0.0, scale)
+        near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], scale)
+    g = np.full(n, 1e37, np.float32)
+    dg, sums = torch.from_numpy(g).cuda(), torch.zeros(3, dtype=torch.float64, device="cuda")
+    plan.norms(dg, sums)
+    for max_norm, taken in ((1e-7, False), (7.1, False), (7.2, True), (100.0, True)):
+        c = O.clip(float(sums[2]), 1.0, max_norm)
+        assert (c >= least) == taken
+        st, step = [torch.from_numpy(p).cuda()] + fresh(torch, plan, n, coded), torch.zeros(1, dtype=torch.int64, device="cuda")
+        old = [a.clone() for a in st]
+        f(B.adamw(lr=1e-3, beta1=B1, beta2=B2, eps=EPS, weight_decay=0.0, max_norm=max_norm), dg, *st, step, d_sumsq=sums)
+        assert int(step) == taken, max_norm
+        if taken:
+            new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1e-3, 0.0, c)
+            near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], max_norm)
+        else:
+            assert all(torch.equal(a, b) for a, b in zip(old, st)), max_norm
