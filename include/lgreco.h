@@ -416,7 +416,7 @@ typedef struct lgreco_optim lgreco_optim_t;
 typedef struct {
     double   lr;            /* >= 0 */
     double   beta1, beta2;  /* in [0, 1) */
-    double   eps;           /* positive and a normal number as fp32 */
+    double   eps;           /* positive and a normal number as fp32, at most 2^126 (about 8.5e37) */
     double   weight_decay;  /* >= 0 */
     double   grad_scale;    /* every gradient is multiplied by it first: 1 / workers behind a sum of their
                              * gradients, 1 / loss scale; positive and a normal number as fp32 */

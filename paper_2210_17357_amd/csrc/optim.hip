@@ -385,7 +385,8 @@ __device__ __forceinline__ Rates rates_of(const StepFactors& f, const StepParams
 // The moments' products and sums are rounded one by one, so that they, and the codes made of them, are what any other fp32
 // program finds (a fused product moves one code in some ten million to its neighbour).
 // The root and the reciprocal are the instructions' (one unit in the last place), which take 8 cycles where the correctly
-// rounded ones take some 50.  The root's takes numbers below 2^-126 for 0: such a v is scaled by 2^64 under it, exactly.
+// rounded ones take some 50.  The root's takes numbers below 2^-126 for 0: such a v is scaled by 2^64 under it, exactly.  The
+// reciprocal's gives 0 for numbers beyond 2^126: no eps is larger, and no root (2^64, its factor 2^27 at most) comes near.
 __device__ __forceinline__ void step_one(const StepParams& k, const Rates& r, float grad, float& p, float& m, float& v) {
     const float g = r.grad * grad;
     m = k.beta1 * m + k.rest1 * g;
@@ -796,7 +797,7 @@ int on_device(lgreco_optim* o) {
 bool valid(const lgreco_adamw_t* c) {
     const auto finite_from = [](double x, double least) { return x >= least && x <= DBL_MAX; };
     return finite_from(c->lr, 0.0) && c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0 &&
-           c->eps <= FLT_MAX && (float)c->eps >= FLT_MIN && finite_from(c->weight_decay, 0.0) && c->grad_scale >= FLT_MIN &&
+           c->eps <= 0x1p126 && (float)c->eps >= FLT_MIN && finite_from(c->weight_decay, 0.0) && c->grad_scale >= FLT_MIN &&
            c->grad_scale <= FLT_MAX && finite_from(c->max_norm, 0.0) && (c->stochastic == 0 || c->stochastic == 1) && c->reserved == 0;
 }
 

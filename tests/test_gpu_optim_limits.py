@@ -146,3 +146,26 @@ def test_the_gradients_factor_is_a_normal_number(coded):
             near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], max_norm)
         else:
             assert all(torch.equal(a, b) for a, b in zip(old, st)), max_norm
+
+
+@pytest.mark.parametrize("coded", [False, True])
+def test_large_eps(coded):
+    """An eps whose reciprocal is a normal number keeps its part of the update; one beyond is refused."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout([700, 3000], 0, 0)
+    rng = np.random.default_rng(24)
+    g = (rng.standard_normal(n) * 1e18).astype(np.float32)
+    p = np.zeros(n, np.float32)
+    plan = B.Optim(table(B, offs, numels))
+    for eps in (1e10, 1e30, 2.0 ** 126, 2.0 ** 126 * (1 + 2.0 ** -23), 2e38, 3.4e38):
+        st, step = [torch.from_numpy(p).cuda()] + fresh(torch, plan, n, coded), torch.zeros(1, dtype=torch.int64, device="cuda")
+        s = B.adamw(lr=1.0, beta1=B1, beta2=B2, eps=eps, weight_decay=0.0)
+        if eps > 2.0 ** 126:
+            with pytest.raises(B.LgrecoError) as e:
+                step_of(plan, coded)(s, torch.from_numpy(g).cuda(), *st, step)
+            assert e.value.status == B.EINVAL
+            continue
+        step_of(plan, coded)(s, torch.from_numpy(g).cuda(), *st, step)
+        new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1.0, 0.0, 1.0, B1, B2, eps)
+        near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], eps)
