@@ -132,6 +132,12 @@ def layer_table(offsets, numels, rows, cols):
     return arr
 
 
+def table_extent(layers) -> int:
+    """Elements that a buffer with the layout of this table has at least."""
+    at = np.frombuffer(layers, np.dtype([("offset", "i8"), ("numel", "i8"), ("shape", "i4", 2)]))
+    return int((at["offset"] + at["numel"]).max())
+
+
 def cand_table(cands: Sequence[Tuple[int, float]]):
     arr = (Cand * len(cands))()
     for i, (f, p) in enumerate(cands):
@@ -408,8 +414,7 @@ class Optim:
         if st != OK:
             raise LgrecoError(st, strerror(st))
         self.L = len(layers)
-        at = np.frombuffer(layers, np.dtype([("offset", "i8"), ("numel", "i8"), ("shape", "i4", 2)]))
-        self.extent = int((at["offset"] + at["numel"]).max())
+        self.extent = table_extent(layers)
         self.blocks = int(lib().lgreco_optim_blocks(self._o))
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         self._f32, self._f64, self._u8, self._i64 = torch.float32, torch.float64, torch.uint8, torch.int64

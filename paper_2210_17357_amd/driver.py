@@ -93,8 +93,20 @@ class AdamW:
 
     def receive(self, handle: "B.Handle", d_payloads, offsets, layers, cands, choice, d_grads, d_lr=None, stream=None):
         """The sum of the workers' payloads into d_grads, then a step on it (settings.grad_scale = 1 / workers makes
-        it the mean).  Layers that travel uncompressed hold their summed gradients in d_grads already."""
-        for w, payload in enumerate(d_payloads):
+        it the mean).  Layers that travel uncompressed hold their summed gradients in d_grads already.  The sum is fp32 whatever
+        gradients `step` takes."""
+        import torch
+        payloads = list(d_payloads)
+        # the receiver's kernels go by the tables alone: what they would write or read past an end is refused in front of them
+        if d_grads.dtype is not torch.float32:
+            raise ValueError("the payloads' sum is fp32, not %s" % d_grads.dtype)
+        need, size = max(self.plan.extent, B.table_extent(layers)), int(offsets[len(layers)])
+        if d_grads.numel() < need:
+            raise ValueError("the tensor has %d elements, %d are needed" % (d_grads.numel(), need))
+        for payload in payloads:
+            if payload.numel() * payload.element_size() < size:
+                raise ValueError("a payload is shorter than its layout (%d bytes)" % size)
+        for w, payload in enumerate(payloads):
             handle.decompress(payload, offsets, layers, cands, choice, d_grads, accumulate=w > 0, stream=stream)
         self.step(d_grads, d_lr=d_lr, stream=stream)
 
