@@ -97,6 +97,8 @@ class AdamW:
         gradients `step` takes."""
         import torch
         payloads = list(d_payloads)
+        if not payloads:
+            raise ValueError("no payloads")
         # the receiver's kernels go by the tables alone: what they would write or read past an end is refused in front of them
         if d_grads.dtype is not torch.float32:
             raise ValueError("the payloads' sum is fp32, not %s" % d_grads.dtype)

@@ -64,3 +64,11 @@ def test_receive_refuses_short_buffers(run):
     with pytest.raises(ValueError):                     # a payload that ends before its last layer's does
         receive(run, PAYLOADS[:1] + [torch.zeros(127, dtype=torch.uint8)], torch.zeros(105))
     assert CALLS == []
+
+
+@pytest.mark.parametrize("none", [[], (), iter(())])
+def test_receive_refuses_no_payloads(run, none):
+    """Without one there is nothing to turn back, and the step would take whatever the buffer holds."""
+    with pytest.raises(ValueError):
+        receive(run, none, torch.zeros(105))
+    assert CALLS == []
