@@ -427,7 +427,9 @@ typedef struct {
 } lgreco_adamw_t;
 
 /* Creates a plan for these layers on the current device.  It takes about 45 bytes of device memory for every 1024 elements
- * and 130 for every layer; tables of more than 2^24 - 1 pieces of 1024 elements (17 G elements): LGRECO_ENOSPACE.
+ * and 130 for every layer; tables of more than 2^24 - 1 pieces of 1024 elements (17 G elements), or
+ * more than the host's memory holds: LGRECO_ENOSPACE; an error of the HIP runtime, device memory that is used up among them: LGRECO_EHIP,
+ * with its text at lgreco_optim_last_hip_error(NULL).
  *   lr_scale     host [L] factors of lr per layer, or NULL (= 1): finite, >= 0
  *   decay_scale  host [L] factors of weight_decay per layer, or NULL (= 1): finite, >= 0 */
 int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int32_t L, const float* lr_scale,
@@ -493,7 +495,8 @@ int lgreco_optim_adamw_coded(lgreco_optim_t* o, const lgreco_adamw_t* cfg, const
 int lgreco_optim_decode(lgreco_optim_t* o, const uint8_t* d_m, const uint8_t* d_v, const uint8_t* d_exps,
                         void* d_m_out, void* d_v_out, int32_t type, void* stream);
 
-/* Text of the last HIP error seen by this plan ("" if none). */
+/* Text of the last HIP error seen by this plan; with NULL, of the one that ended the calling thread's last creation of a
+ * plan ("" if none). */
 const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o);
 
 const char* lgreco_strerror(int status);

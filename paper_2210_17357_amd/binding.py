@@ -412,7 +412,7 @@ class Optim:
         st = lib().lgreco_optim_create(C.byref(self._o), C.addressof(layers), len(layers),
                                        *(None if a is None else _np(a) for a in scales))
         if st != OK:
-            raise LgrecoError(st, strerror(st))
+            self._failed(st)
         self.L = len(layers)
         self.extent = table_extent(layers)
         self.blocks = int(lib().lgreco_optim_blocks(self._o))

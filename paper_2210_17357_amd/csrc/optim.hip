@@ -691,6 +691,9 @@ struct lgreco_optim {
 
 namespace {
 
+// Text of the HIP error that ended this thread's last creation of a plan, which leaves no plan to ask ("": none did).
+thread_local char create_error[sizeof(lgreco_optim::error)] = "";
+
 int hip_fail(lgreco_optim* o, hipError_t e, const char* what) {
     std::snprintf(o->error, sizeof(o->error), "%s: %s", what, hipGetErrorString(e));
     return LGRECO_EHIP;
@@ -847,6 +850,7 @@ int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int3
                         const float* decay_scale) {
     if (!out) return LGRECO_EINVAL;
     *out = nullptr;
+    create_error[0] = 0;
     lgreco_optim* o = new (std::nothrow) lgreco_optim();
     if (!o) return LGRECO_ENOSPACE;
     int st;
@@ -855,8 +859,12 @@ int lgreco_optim_create(lgreco_optim_t** out, const lgreco_layer_t* layers, int3
     } catch (...) {                                          // (host memory)
         st = LGRECO_ENOSPACE;
     }
-    if (st == LGRECO_OK) *out = o;
-    else lgreco_optim_destroy(o);
+    if (st == LGRECO_OK) {
+        *out = o;
+    } else {
+        std::memcpy(create_error, o->error, sizeof(create_error));
+        lgreco_optim_destroy(o);
+    }
     return st;
 }
 
@@ -869,7 +877,7 @@ int lgreco_optim_destroy(lgreco_optim_t* o) {
 
 int64_t lgreco_optim_blocks(const lgreco_optim_t* o) { return o ? o->blocks : -1; }
 
-const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o) { return o ? o->error : ""; }
+const char* lgreco_optim_last_hip_error(const lgreco_optim_t* o) { return o ? o->error : create_error; }
 
 int lgreco_optim_norms(lgreco_optim_t* o, const void* d_grads, int32_t grad_type, double* d_sumsq, void* stream) {
     if (!o || !d_grads || !d_sumsq || !gradient_type(grad_type)) return LGRECO_EINVAL;
