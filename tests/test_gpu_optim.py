@@ -1,8 +1,9 @@
 """GPU: norms, AdamW with fp32 moments and with moments in 8 bits against the step in 64 bits.
 
 Errors are counted in u = 2^-24, half a step of fp32.  With g = c * grad rounded twice (c, the product): 2 u of it.
-  m' = fma(b1, m, r1 * g): b1 and r1 are rounded, so u of b1 m and 4 u of r1 g, and u of the sum: at most 6 u (|b1 m| + |r1 g|)
-  v' = fma(b2, v, r2 * (g * g)): u of b2 v, 4 + 1 + 1 + 1 u of r2 g^2, and u of the sum: at most 9 u v'
+  m' = b1 * m + r1 * g: b1 and r1, both products and the sum are rounded, so 2 u of b1 m and 4 u of r1 g, and u of the sum:
+  at most 6 u (|b1 m| + |r1 g|)
+  v' = b2 * v + r2 * (g * g): 2 u of b2 v, 4 + 1 + 1 + 1 u of r2 g^2, and u of the sum: at most 9 u v'
   update m' / (sqrt(v') * root + eps): half of v's 9 u, the root's u, the factor's and the sum's rounding and eps's: 9 u of
   the denominator, u of the quotient, 2 u of the rate and its product
   p' = p - (shrink * p + rate * update): 2 u of the first term, 1 u more of the second, u of p'

@@ -169,3 +169,51 @@ def test_large_eps(coded):
         step_of(plan, coded)(s, torch.from_numpy(g).cuda(), *st, step)
         new, tol = bounds(g, p, np.zeros(n), np.zeros(n), 1, 1.0, 0.0, 1.0, B1, B2, eps)
         near(st[0].cpu().numpy()[:3700], new[0][:3700], tol[0][:3700], eps)
+
+
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_moments_are_rounded_operation_by_operation(kind, coded):
+    """m' and v' bit for bit those of fp32 arithmetic that rounds the factors, every product and every sum, over three steps; with 8 bits
+    the codes and exponents of exactly those numbers.  The inputs tell a fused product and sum apart."""
+    from paper_2210_17357_amd import binding as B
+    torch = torch_cuda()
+    offs, numels, n = layout(*TABLES["parts"])
+    rng = np.random.default_rng(25)
+    inside = np.zeros(n, bool)
+    for o, k in zip(offs, numels):
+        inside[o:o + k] = True
+    plan = B.Optim(table(B, offs, numels))
+    f32 = np.float32
+    b1, r1, b2, r2, c = (f32(x) for x in (B1, 1.0 - B1, B2, 1.0 - B2, 1 / 3))
+    s = B.adamw(lr=1e-3, beta1=B1, beta2=B2, eps=EPS, grad_scale=1 / 3)
+    st, dp, step = fresh(torch, plan, n, coded), torch.zeros(n, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    for t in (1, 2, 3):
+        dg = typed(torch, (rng.standard_normal(n) * 10.0 ** rng.uniform(-4, 0, n)).astype(f32), kind)
+        old = [a.astype(f32) for a in held(st, offs, numels, coded)]
+        step_of(plan, coded)(s, dg, dp, *st, step)
+        g = c * exact_grads(torch, dg.float().cpu().numpy(), "f32").astype(f32)
+        want = [b1 * old[0] + r1 * g, b2 * old[1] + r2 * (g * g)]
+        if t > 1:
+            wide = (b1 * old[0].astype(np.float64) + (r1 * g)).astype(f32)          # the first product not rounded
+            assert ((wide != want[0]) & inside).any()
+            wide = (b2 * old[1].astype(np.float64) + r2 * (g * g)).astype(f32)
+            assert ((wide != want[1]) & inside).any()
+        got = held(st, offs, numels, coded)
+        if not coded:
+            for a, w, what in zip(got, want, "mv"):
+                assert np.array_equal(a[inside], w[inside]), (what, t)
+            continue
+        exps, first = st[2].cpu().numpy().reshape(-1, 2), 0
+        for o, k in zip(offs, numels):
+            for j in range(0, k, 128):
+                cut, x = slice(o + j, o + min(j + 128, k)), exps[first]
+                first += 1
+                for q, octaves in ((0, O.OCTAVES_M), (1, O.OCTAVES_V)):
+                    a = np.abs(want[q][cut])
+                    assert O.exponent(a) == x[q]
+                    keep = O.rounded(a, int(x[q]), octaves)
+                    if q:
+                        keep = np.where(a > 0, np.maximum(keep, 2.0 ** (int(x[q]) - 127.0 - 14 - 4)), keep)
+                    assert np.array_equal(np.abs(got[q][cut]), keep), (q, t, o, j)
+                    assert (np.sign(got[q][cut]) * np.sign(want[q][cut]) >= 0).all()
