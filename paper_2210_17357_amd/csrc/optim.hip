@@ -19,8 +19,9 @@ namespace {
 
 constexpr int kOptimBlock = LGRECO_OPTIM_BLOCK;
 // Elements of a workgroup of the norms, doubled while there would be more than kNormParts: enough workgroups to fill the chip
-// more than once, few enough partial sums (355 M elements, us: 16384 a workgroup 215, 65536 213, 131072 212, 262144 232; of bf16 133, 138,
-// 164; 67 M of bf16: 38, 49, 75 and 130, with 32768 36; 25 M: 22, 24, 30, 47).
+// more than once, few enough partial sums.  One layer, us with 16384 / 32768 / 65536 / 131072 / 262144: 355 M elements of fp32 223 / 220 / 217 /
+// 225 / 222, of bf16 118 / 114 / 114 / 115 / 116; 67 M 49 / 46 / 44 / 43 / 49 and 27 / 27 / 26 / 25 / 31; 25.6 M 20 / 22 / 19 / 27 / 44
+// and 13 / 14 / 13 / 18 / 28; 4.8 M 8.3 / 9.8 / 13 / 21 / 36 and 7.1 / 8.0 / 11 / 15 / 25.  (Smaller ones are not measured.)
 constexpr int kNormPart = 16384, kNormParts = 6000;
 constexpr int kStepPart = 4 * kThreads;        // elements of a workgroup of the step: one access a thread and buffer
 // With 8-bit moments a thread takes 8 elements, and workgroups are half as large where short layers would leave more than a quarter
@@ -31,7 +32,9 @@ constexpr int kShortParts = 65536;             // most workgroups of a step that
 // Longer steps ask for LDS that they do not use, so that 3 workgroups (5 with 8-bit moments) share a compute unit and not 8: the
 // chip's accesses then stay in a narrower window of memory.  355 M elements, us, with 8 / 6 / 5 / 4 / 3 / 2: fp32 moments
 // 1730 / 1685 / 1650 / 1640 / 1615 / 1675, 8-bit ones 990 / 978 / 933 / 928 / 980 / 1258; 150 M 741 / 721 / 700 / 697 / 682 /
-// 682 and 411 / 397 / 409 / 404 / 421 / 515.  Below 80 M elements it makes no difference.
+// 682 and 411 / 397 / 409 / 404 / 421 / 515.  Below 80 M elements it makes no difference.  These are workgroups of long layers, full
+// ones.  The limit goes by their number alone, and costs where layers are short (us a step, with / without, fp32 moments and 8-bit ones): 70000
+// layers of 400 elements 174 / 153 and 202 / 118, 40000 of 2100 399 / 419 and 302 / 275.
 constexpr size_t kStepLds = 52 << 10, kCodedLds = 31 << 10;
 constexpr int64_t kMaxParts = ((int64_t)1 << 32) / kThreads - 1;   // (a launch takes fewer than 2^32 threads)
 constexpr int kLine = 32;            // elements of a 128-byte line of fp32
@@ -220,7 +223,7 @@ __device__ __forceinline__ double sum_published(const double* p, int n, double* 
     return sum_of_waves(a, s_sum);
 }
 
-// Bound by HBM: 355 M elements of fp32 in 216 us (6.6 TB/s), of bf16 in 114 (6.2).  The last workgroup of a layer adds up the layer's partial sums, the last of those the layers' sums.
+// Bound by HBM: 355 M elements of fp32 in 217 us (6.5 TB/s), of bf16 in 114-119 (6.0-6.2).  The last workgroup of a layer adds up the layer's partial sums, the last of those the layers' sums.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void norms_kernel(NormParams k) {
     __shared__ double s_sum[3][kThreads / 64];
@@ -501,7 +504,7 @@ __device__ __forceinline__ void decode8(const uint32_t (&cm)[2], const uint32_t 
     }
 }
 
-// Bound by HBM: 355 M elements with bf16 gradients and copy, stochastic, in 932 us (16 bytes each: 6.1 TB/s); rounding to nearest
+// Bound by HBM: 355 M elements with bf16 gradients and copy, stochastic, in 936 us (16 bytes each: 6.1 TB/s); rounding to nearest
 // takes as long.  A row of 16 lanes takes a block, so that its maxima take four vector instructions each and no LDS.  (Lanes with 8
 // consecutive elements, whose fp32 accesses are half lines: 1100; the codes' accesses with streaming hints: 1 to 3 % more.)
 template <typename G, typename C, bool STOCHASTIC>
@@ -603,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void adamw_coded_kernel(StepParams k) {
 }
 
 // Bound by HBM.  A row of 16 lanes takes a block; for 16-bit values a lane takes 8 consecutive elements, one access of each
-// buffer (355 M elements: 360 us, 5.9 TB/s, 390 as for fp32).
+// buffer (355 M elements: 361 us, 5.9 TB/s, 390 in the places of fp32; fp32 values 568 us, 6.2 TB/s).
 template <typename O>
 __global__ __launch_bounds__(kThreads) void moments_kernel(const CodedPart* __restrict__ parts, const uint8_t* __restrict__ codes_m,
                                                            const uint8_t* __restrict__ codes_v, const uint8_t* __restrict__ exps,
